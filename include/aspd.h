@@ -211,6 +211,46 @@ ASPD_API int aspd_renumber_branches(const aspd_state* state, const int32_t* new_
 ASPD_API int aspd_rope_append(const aspd_kv* kv, const aspd_step* step, void* q_d, const void* k_new_d,
                               const void* v_new_d, float rope_theta, void* stream);
 
+/* The same step for models that norm every query and key head before the rotation, or whose positions have several axes
+ * (time, height and width of images and video), or whose scores are biased by distance (aspd_scores), on rows as a fused
+ * projection leaves them.  For every new token r of `step`:
+ *   every head x of the queries (with q_weight_d) and keys (with k_weight_d):
+ *     x <- x / sqrt(mean(x^2) + norm_eps) * (weight_offset + weight);
+ *   pair (i, i + head_dim/2) of every query and key head turns by p * rope_theta^(-2i/head_dim), where
+ *     p = axis_pos[axis_of_pair[i]][r]                                        with axis_pos_d,
+ *     p = position_ids[r] + pos_offset[sequence of r] on every axis           with pos_offset_d,
+ *     p = position_ids[r]                                                     with neither;
+ *   the query goes to q_out_d[r], the key and the value as it is to the cache at slot_mapping[r];
+ *   position_ids[r], the token's place in Eq. 4, goes to slot_pos_d[sequence][logical slot] (with slot_pos_d), where the
+ *     distance bias of aspd_scores reads it.
+ * Row r of q is q_d + r * q_stride elements, [num_q_heads][head_dim] in kv->dtype, and likewise k and v with num_kv_heads;
+ * a stride of 0 stands for rows packed one behind the other, others are at least a row.  q_out_d is packed, as the attention
+ * calls take it; it may be q_d itself where that is packed, NULL writes the queries where they stand, at their stride.
+ * Otherwise the arrays must not overlap.  Arithmetic in fp32 (sums of squares too), angles in fp64; bf16 results are
+ * rounded once, to nearest even.  Rows that the metadata call dropped (see aspd_state.fault_d) are written nowhere outside
+ * the arrays, as in aspd_rope_append. */
+#define ASPD_MAX_AXES 4
+typedef struct aspd_rotary {
+  float          rope_theta;     /* > 1; 0: nothing turns (models whose scores are biased by distance instead)       */
+  int32_t        num_axes;       /* with axis_pos_d: 1 .. ASPD_MAX_AXES; ignored without                             */
+  const int32_t* axis_pos_d;     /* nullable [num_axes][axis_stride]: positions of the step's rows on every axis     */
+  int64_t        axis_stride;    /* >= step->NQ                                                                      */
+  const uint8_t* axis_of_pair;   /* HOST, [head_dim / 2], each < num_axes: which axis a pair turns by; NULL: axis 0.
+                                    Read with axis_pos_d only                                                        */
+  const int32_t* pos_offset_d;   /* nullable [B]: how far a sequence's positions lie behind (< 0) or ahead of its
+                                    position ids, for tokens that have one position on all axes: a text that goes on
+                                    behind an image.  Not together with axis_pos_d                                   */
+  const void*    q_weight_d;     /* nullable [head_dim] in kv->dtype: queries are normed                              */
+  const void*    k_weight_d;     /* nullable [head_dim] in kv->dtype: keys are normed                                 */
+  float          norm_eps;       /* > 0 where a weight is given                                                      */
+  float          weight_offset;  /* 0, or 1 for weights that are kept as their distance from one; finite             */
+} aspd_rotary;
+/* `state`: its B and owner_stride size pos_offset_d and slot_pos_d ([B][owner_stride]); may be NULL without both. */
+ASPD_API int aspd_norm_rope_append(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                   const aspd_rotary* how, void* q_d, int64_t q_stride, const void* k_new_d,
+                                   int64_t k_stride, const void* v_new_d, int64_t v_stride, void* q_out_d,
+                                   int32_t* slot_pos_d, void* stream);
+
 /* Bytes of device scratch the attention calls of a step with NQ rows need at most: arrival counters, room
  * for a plan, and the partial softmax results of split key ranges (host-only computation; sized for the
  * current device's compute units, for 256 of them when there is no device).  Returns 0 on invalid arguments. */
@@ -308,6 +348,35 @@ ASPD_API int aspd_build_sequence_meta(const aspd_kv* kv, aspd_state* state, cons
 ASPD_API int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
                                      const void* q_d, void* out_d, float* lse_d, float sm_scale,
                                      void* workspace_d, size_t workspace_bytes, void* stream);
+
+/* ---- Attention on changed scores --------------------------------------------------------------------
+ * The four calls above for models that cap their scores, or bias them by distance, or both.  The score of query row r and
+ * the key in slot j is, with s = sm_scale * q.k,
+ *   s <- softcap * tanh(s / softcap)                                 where softcap > 0, and then
+ *   s <- s + slopes[query head] * (slot_pos[sequence][j] - position_ids[r])    where slopes_d is given.
+ * Which keys a row sees, the softmax over them and lse_d (of the changed scores) are those of the call named, and so are
+ * all other arguments, the step's plan and the workspace.  Distances are those of Eq. 4's position ids, so that a branch is
+ * biased as if it were alone behind the prefix: slot_pos_d[sequence][slot] holds the position id of the token in each slot
+ * that is in use (aspd_norm_rope_append writes it; of slots not in use nothing is used).  Positions and their differences
+ * lie within +- 2^24.  Scores are formed in fp32. */
+typedef struct aspd_scores {
+  float          softcap;     /* 0: none; otherwise 2^-10 .. 2^10 (ASPD_ERR_UNSUPPORTED outside)                         */
+  const float*   slopes_d;    /* nullable [num_q_heads], finite: usually positive, so that a far key (a negative
+                                 difference) counts less                                                              */
+  const int32_t* slot_pos_d;  /* with slopes_d: [B][owner_stride], owner_stride at least max_blocks_per_seq * 16        */
+} aspd_scores;
+ASPD_API int aspd_attn_parallel_decode_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                              const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d,
+                                              float sm_scale, void* workspace_d, size_t workspace_bytes, void* stream);
+ASPD_API int aspd_attn_branch_chunk_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                           const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d,
+                                           float sm_scale, void* workspace_d, size_t workspace_bytes, void* stream);
+ASPD_API int aspd_attn_serial_decode_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                            const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d,
+                                            float sm_scale, void* workspace_d, size_t workspace_bytes, void* stream);
+ASPD_API int aspd_attn_full_sequence_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                            const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d,
+                                            float sm_scale, void* workspace_d, size_t workspace_bytes, void* stream);
 
 /* aspd_attn_parallel_decode for callers that cannot allocate device memory (code under HIP graph
  * capture, tight serving loops, harnesses that forbid hipMalloc): same arguments without the workspace,

@@ -31,8 +31,9 @@ FAULT_LAYOUT = 64
 EXPORTS = ("aspd_build_branch_meta", "aspd_renumber_branches", "aspd_rope_append", "aspd_plan_bytes",
            "aspd_workspace_bytes", "aspd_workspace_init", "aspd_attn_parallel_decode",
            "aspd_attn_branch_chunk", "aspd_attn_serial_decode", "aspd_attn_parallel_decode_static",
-           "aspd_sequence_plan_bytes", "aspd_build_sequence_meta", "aspd_attn_full_sequence",
-           "aspd_probe_read_bandwidth", "aspd_status_string")
+           "aspd_sequence_plan_bytes", "aspd_build_sequence_meta", "aspd_attn_full_sequence", "aspd_norm_rope_append",
+           "aspd_attn_parallel_decode_scored", "aspd_attn_branch_chunk_scored", "aspd_attn_serial_decode_scored",
+           "aspd_attn_full_sequence_scored", "aspd_probe_read_bandwidth", "aspd_status_string")
 
 
 class aspd_kv(C.Structure):
@@ -60,6 +61,16 @@ class aspd_step(C.Structure):
 class aspd_layout(C.Structure):
     _fields_ = [("num_runs", C.c_int32), ("cu_runs_d", C.c_void_p), ("run_branch_d", C.c_void_p),
                 ("run_len_d", C.c_void_p)]
+
+
+class aspd_rotary(C.Structure):
+    _fields_ = [("rope_theta", C.c_float), ("num_axes", C.c_int32), ("axis_pos_d", C.c_void_p), ("axis_stride", C.c_int64),
+                ("axis_of_pair", C.c_void_p), ("pos_offset_d", C.c_void_p), ("q_weight_d", C.c_void_p),
+                ("k_weight_d", C.c_void_p), ("norm_eps", C.c_float), ("weight_offset", C.c_float)]
+
+
+class aspd_scores(C.Structure):
+    _fields_ = [("softcap", C.c_float), ("slopes_d", C.c_void_p), ("slot_pos_d", C.c_void_p)]
 
 
 class AspdError(RuntimeError):
@@ -104,6 +115,16 @@ def lib() -> C.CDLL:
         L.aspd_attn_parallel_decode_static.restype = C.c_int
         L.aspd_attn_parallel_decode_static.argtypes = [C.POINTER(aspd_kv), C.POINTER(aspd_state), C.POINTER(aspd_step),
                                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p]
+        for name in ("aspd_attn_parallel_decode_scored", "aspd_attn_branch_chunk_scored", "aspd_attn_serial_decode_scored",
+                     "aspd_attn_full_sequence_scored"):
+            fn = getattr(L, name)
+            fn.restype = C.c_int
+            fn.argtypes = [C.POINTER(aspd_kv), C.POINTER(aspd_state), C.POINTER(aspd_step), C.POINTER(aspd_scores),
+                           C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.aspd_norm_rope_append.restype = C.c_int
+        L.aspd_norm_rope_append.argtypes = [C.POINTER(aspd_kv), C.POINTER(aspd_state), C.POINTER(aspd_step),
+                                            C.POINTER(aspd_rotary), C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                            C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]
         L.aspd_workspace_init.restype = C.c_int
         L.aspd_workspace_init.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p]
         L.aspd_probe_read_bandwidth.restype = C.c_int
@@ -160,6 +181,45 @@ class KVCache:
                        self.block_tables.shape[1], _DTYPE[self.k.dtype])
 
 
+@dataclass
+class Rotary:
+    """How aspd_norm_rope_append norms and turns queries and keys, see aspd_rotary in aspd.h: axis_pos [axes][rows] and
+    pos_offset [B] int32, weights [head_dim] of the cache's type, axis_of_pair any sequence of head_dim / 2 axes (kept as
+    bytes; axes_in_sections and axes_in_turn make the customary ones)."""
+    rope_theta: float
+    axis_of_pair: bytes | None = None
+    axis_pos: torch.Tensor | None = None
+    pos_offset: torch.Tensor | None = None
+    q_weight: torch.Tensor | None = None
+    k_weight: torch.Tensor | None = None
+    norm_eps: float = 1e-6
+    weight_offset: float = 0.0
+
+    def __post_init__(self):
+        if self.axis_of_pair is not None:
+            self.axis_of_pair = bytes(int(a) for a in self.axis_of_pair)
+
+
+def axes_in_sections(pairs) -> bytes:
+    """axis_of_pair: the first pairs[0] pairs of a head turn by axis 0, the next pairs[1] by axis 1, and so on."""
+    return b"".join(bytes([axis]) * int(n) for axis, n in enumerate(pairs))
+
+
+def axes_in_turn(pairs) -> bytes:
+    """axis_of_pair: the axes take turns, each until it has had its pairs[axis]; axis 0 has what is left."""
+    axes, total = len(pairs), sum(int(n) for n in pairs)
+    return bytes(i % axes if i < axes * int(pairs[i % axes]) else 0 for i in range(total))
+
+
+@dataclass
+class Scores:
+    """Changed scores of the attention calls, see aspd_scores in aspd.h: slopes [num_q_heads] float32, slot_pos
+    [B][owner_stride] int32 (new_slot_pos; aspd_norm_rope_append fills it)."""
+    softcap: float = 0.0
+    slopes: torch.Tensor | None = None
+    slot_pos: torch.Tensor | None = None
+
+
 class BatchState:
     """Caller-owned decode state of a batch (device int arrays), see aspd_state in aspd.h."""
 
@@ -190,6 +250,11 @@ class BatchState:
         return aspd_state(self.B, self.NB, _ptr(self.stage_base), _ptr(self.seq_len), _ptr(self.cu_branches),
                           _ptr(self.branch_len), _ptr(self.slot_owner), self.owner_stride, _ptr(self.fault),
                           _ptr(self.main_pos), _ptr(self.stage_open))
+
+
+def new_slot_pos(state: BatchState) -> torch.Tensor:
+    """Position ids of the slots of a batch, as aspd_norm_rope_append writes and aspd_scores reads them."""
+    return torch.zeros(state.B, state.owner_stride, dtype=torch.int32, device=state.device)
 
 
 class Step:
@@ -269,6 +334,17 @@ def aspd_rope_append(kv: KVCache, step: Step, q: torch.Tensor, k_new: torch.Tens
     return q
 
 
+def aspd_norm_rope_append(kv: KVCache, state: BatchState, step: Step, rotary: Rotary, q: torch.Tensor, k_new: torch.Tensor,
+                          v_new: torch.Tensor, q_out: torch.Tensor | None = None, slot_pos: torch.Tensor | None = None,
+                          stream=None) -> torch.Tensor:
+    """See aspd.h.  q, k_new, v_new: [rows][heads][head_dim], rows at any stride (slices of one projection).  Queries go to
+    q_out (packed, as the attention calls take them), without one they are written where they stand.  Returns them."""
+    rc = _calls().norm_rope_append(kv, state, step, rotary, q, k_new, v_new, q_out, slot_pos, stream)
+    if rc != OK:
+        raise AspdError(rc, "aspd_norm_rope_append")
+    return q if q_out is None else q_out
+
+
 def aspd_workspace_bytes(kv: KVCache, B: int, NQ: int) -> int:
     kvs = kv.struct()
     return int(lib().aspd_workspace_bytes(C.byref(kvs), B, NQ))
@@ -284,25 +360,31 @@ _ATTN = ("aspd_attn_parallel_decode", "aspd_attn_branch_chunk", "aspd_attn_seria
          "aspd_attn_parallel_decode_static")
 
 
-def _attn(which, kv, state, step, q, out, lse, sm_scale, workspace, stream):
+def _attn(which, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores=None):
     if out is None and which != 4:   # (the static call allocates nothing and refuses to go without)
         out = torch.empty_like(q)
-    rc = _calls().attn(which, kv, state, step, q, out, lse, sm_scale, workspace, stream)
+    if scores is None:
+        rc = _calls().attn(which, kv, state, step, q, out, lse, sm_scale, workspace, stream)
+    else:
+        rc = _calls().attn_scored(which, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores)
     if rc != OK:
-        raise AspdError(rc, _ATTN[which])
+        raise AspdError(rc, _ATTN[which] if scores is None else _ATTN[which] + "_scored")
     return out
 
 
-def aspd_attn_parallel_decode(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None):
-    return _attn(0, kv, state, step, q, out, lse, sm_scale, workspace, stream)
+# With `scores` (a Scores) the calls go to the library's entry points of the same name and `_scored`.
 
 
-def aspd_attn_branch_chunk(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None):
-    return _attn(1, kv, state, step, q, out, lse, sm_scale, workspace, stream)
+def aspd_attn_parallel_decode(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None, scores=None):
+    return _attn(0, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores)
 
 
-def aspd_attn_serial_decode(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None):
-    return _attn(2, kv, state, step, q, out, lse, sm_scale, workspace, stream)
+def aspd_attn_branch_chunk(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None, scores=None):
+    return _attn(1, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores)
+
+
+def aspd_attn_serial_decode(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None, scores=None):
+    return _attn(2, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores)
 
 
 def aspd_sequence_plan_bytes(kv: KVCache, B: int, NQ: int) -> int:
@@ -326,8 +408,8 @@ def aspd_build_sequence_meta(kv: KVCache, state: BatchState, cu_runs: torch.Tens
     return step
 
 
-def aspd_attn_full_sequence(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None):
-    return _attn(3, kv, state, step, q, out, lse, sm_scale, workspace, stream)
+def aspd_attn_full_sequence(kv, state, step, q, workspace, out=None, lse=None, sm_scale=0.0, stream=None, scores=None):
+    return _attn(3, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores)
 
 
 def aspd_attn_parallel_decode_static(kv, state, step, q, out, lse=None, sm_scale=0.0, stream=None):

@@ -93,8 +93,26 @@ bool merge_apart(const aspd_kv* kv, int B, int NQ, int max_new_per_seq, const At
 
 enum Mode { MODE_PARALLEL, MODE_CHUNK, MODE_SERIAL };
 
-int attn_launch(Mode mode, const aspd_kv* kv, const aspd_state* state, const aspd_step* step, const void* q_d,
-                void* out_d, float* lse_d, float sm_scale, void* workspace_d, size_t workspace_bytes,
+// What a call on changed scores brings beyond the call of the same name (scores: null for that one).
+int check_scores(const aspd_kv* kv, const aspd_state* state, const aspd_step* step, const aspd_scores* scores) {
+  if (!(scores->softcap >= 0.f) || !std::isfinite(scores->softcap)) return ASPD_ERR_INVALID_ARG;
+  if (scores->softcap != 0.f && (scores->softcap < 0x1p-10f || scores->softcap > 0x1p10f)) return ASPD_ERR_UNSUPPORTED;
+  if (scores->slopes_d && (!scores->slot_pos_d || !step->position_ids_d || state->owner_stride < kv->max_blocks_per_seq * ASPD_BLOCK))
+    return ASPD_ERR_INVALID_ARG;
+  return ASPD_OK;
+}
+void set_scores(AttnArgs* a, const aspd_state* state, const aspd_step* step, const aspd_scores* scores) {
+  const bool cap = scores && scores->softcap > 0.f, bias = scores && scores->slopes_d;
+  a->cap_in = cap ? 2.f * a->scale_log2 / scores->softcap : 0.f;
+  a->cap_log2 = cap ? scores->softcap * LOG2E : 0.f;
+  a->slopes = bias ? scores->slopes_d : nullptr;
+  a->slot_pos = bias ? scores->slot_pos_d : nullptr;
+  a->pos_stride = bias ? state->owner_stride : 0;
+  a->position_ids = bias ? step->position_ids_d : nullptr;
+}
+
+int attn_launch(Mode mode, const aspd_kv* kv, const aspd_state* state, const aspd_step* step, const aspd_scores* scores,
+                const void* q_d, void* out_d, float* lse_d, float sm_scale, void* workspace_d, size_t workspace_bytes,
                 void* stream) {
   int rc = aspd_check_kv(kv);
   if (rc != ASPD_OK) return rc;
@@ -106,6 +124,7 @@ int attn_launch(Mode mode, const aspd_kv* kv, const aspd_state* state, const asp
   if (!step->q_branch_d || !step->logical_slot_d || !q_d || !out_d) return ASPD_ERR_INVALID_ARG;
   if (((uintptr_t)q_d & 15) || ((uintptr_t)out_d & 15)) return ASPD_ERR_INVALID_ARG;
   if (!(sm_scale >= 0.f)) return ASPD_ERR_INVALID_ARG;
+  if (scores && (rc = check_scores(kv, state, step, scores)) != ASPD_OK) return rc;
   const bool branches = (mode != MODE_SERIAL) && step->shared_mask == 0;  // rows that may carry branch tags
   if (branches) {
     if (!state->cu_branches_d || !state->slot_owner_d) return ASPD_ERR_INVALID_ARG;
@@ -152,6 +171,7 @@ int attn_launch(Mode mode, const aspd_kv* kv, const aspd_state* state, const asp
   a.merge_apart = 0;
   a.NQ = step->NQ;
   a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : sm_scale) * LOG2E;
+  set_scores(&a, state, step, scores);
   a.B = state->B;
   a.nwg = v.nwg;
   a.G = kv->num_q_heads / kv->num_kv_heads;
@@ -169,13 +189,23 @@ int attn_launch(Mode mode, const aspd_kv* kv, const aspd_state* state, const asp
     ASPD_HIP_CHECK(hipGetLastError());                                               \
   } while (0)
   a.merge_apart = merge_apart(kv, state->B, step->NQ, step->max_new_per_seq, v);
+  // The kernels are built once for the scores as they are and once for each way to change them.
+#define ASPD_CHANGED(LAUNCH)                                  \
+  do {                                                        \
+    if (a.cap_log2 == 0.f && !a.slopes) LAUNCH(false, false); \
+    else if (!a.slopes) LAUNCH(true, false);                  \
+    else if (a.cap_log2 == 0.f) LAUNCH(false, true);          \
+    else LAUNCH(true, true);                                  \
+  } while (0)
   if (v.kernel == KERNEL_BF16_ROWS) {
-    if (D == 128)
-      ASPD_LAUNCH((attn_bf16_rows_kernel<128, ROWS_NW>), ROWS_NW * 64,
-                  (rows_smem_bytes<128>()));
-    else
-      ASPD_LAUNCH((attn_bf16_rows_kernel<64, ROWS_NW>), ROWS_NW * 64,
-                  (rows_smem_bytes<64>()));
+#define ASPD_ROWS_128(CAP, BIAS) \
+  ASPD_LAUNCH((attn_bf16_rows_kernel<128, ROWS_NW, CAP, BIAS>), ROWS_NW * 64, (rows_smem_bytes<128, BIAS>()))
+#define ASPD_ROWS_64(CAP, BIAS) \
+  ASPD_LAUNCH((attn_bf16_rows_kernel<64, ROWS_NW, CAP, BIAS>), ROWS_NW * 64, (rows_smem_bytes<64, BIAS>()))
+    if (D == 128) ASPD_CHANGED(ASPD_ROWS_128);
+    else ASPD_CHANGED(ASPD_ROWS_64);
+#undef ASPD_ROWS_128
+#undef ASPD_ROWS_64
     if (a.merge_apart) {
       if (D == 128) hipLaunchKernelGGL(merge_kernel<128>, dim3(a.nwg), dim3(MERGE_THREADS), 0, hs, a);
       else hipLaunchKernelGGL(merge_kernel<64>, dim3(a.nwg), dim3(MERGE_THREADS), 0, hs, a);
@@ -183,26 +213,37 @@ int attn_launch(Mode mode, const aspd_kv* kv, const aspd_state* state, const asp
     }
   } else if (v.kernel == KERNEL_BF16_STREAM) {
     // pages that no second row group reads are fetched with non-temporal loads
-#define ASPD_BF16_CASE(DD, NN)                                                                            \
-  do {                                                                                                    \
-    if (v.stream_once)                                                                                    \
-      ASPD_LAUNCH((attn_bf16_kernel<DD, NN, true>), STREAM_NW * 64, (StreamLds<DD, NN>::BYTES));          \
-    else                                                                                                  \
-      ASPD_LAUNCH((attn_bf16_kernel<DD, NN, false>), STREAM_NW * 64, (StreamLds<DD, NN>::BYTES));         \
+#define ASPD_STREAM(DD, NN, CAP, BIAS)                                                                               \
+  do {                                                                                                               \
+    if (v.stream_once)                                                                                               \
+      ASPD_LAUNCH((attn_bf16_kernel<DD, NN, true, CAP, BIAS>), STREAM_NW * 64, (StreamLds<DD, NN, BIAS>::BYTES));    \
+    else                                                                                                             \
+      ASPD_LAUNCH((attn_bf16_kernel<DD, NN, false, CAP, BIAS>), STREAM_NW * 64, (StreamLds<DD, NN, BIAS>::BYTES));   \
   } while (0)
-    if (D == 128) {
-      if (v.nt == 1) ASPD_BF16_CASE(128, 1);
-      else if (v.nt == 2) ASPD_BF16_CASE(128, 2);
-      else ASPD_BF16_CASE(128, 3);
-    } else {
-      if (v.nt == 1) ASPD_BF16_CASE(64, 1);
-      else if (v.nt == 2) ASPD_BF16_CASE(64, 2);
-      else ASPD_BF16_CASE(64, 3);
-    }
+#define ASPD_BF16_CASE(CAP, BIAS)                              \
+  do {                                                         \
+    if (D == 128) {                                            \
+      if (v.nt == 1) ASPD_STREAM(128, 1, CAP, BIAS);           \
+      else if (v.nt == 2) ASPD_STREAM(128, 2, CAP, BIAS);      \
+      else ASPD_STREAM(128, 3, CAP, BIAS);                     \
+    } else {                                                   \
+      if (v.nt == 1) ASPD_STREAM(64, 1, CAP, BIAS);            \
+      else if (v.nt == 2) ASPD_STREAM(64, 2, CAP, BIAS);       \
+      else ASPD_STREAM(64, 3, CAP, BIAS);                      \
+    }                                                          \
+  } while (0)
+    ASPD_CHANGED(ASPD_BF16_CASE);
 #undef ASPD_BF16_CASE
+#undef ASPD_STREAM
   } else {
-    if (D == 128) ASPD_LAUNCH(attn_f32_kernel<128>, THREADS, f32_smem_bytes<128>());
-    else ASPD_LAUNCH(attn_f32_kernel<64>, THREADS, f32_smem_bytes<64>());
+    const bool changed = a.cap_log2 > 0.f || a.slopes;
+    if (D == 128) {
+      if (changed) ASPD_LAUNCH((attn_f32_kernel<128, true>), THREADS, (f32_smem_bytes<128, true>()));
+      else ASPD_LAUNCH((attn_f32_kernel<128, false>), THREADS, (f32_smem_bytes<128, false>()));
+    } else {
+      if (changed) ASPD_LAUNCH((attn_f32_kernel<64, true>), THREADS, (f32_smem_bytes<64, true>()));
+      else ASPD_LAUNCH((attn_f32_kernel<64, false>), THREADS, (f32_smem_bytes<64, false>()));
+    }
   }
 #undef ASPD_LAUNCH
   return ASPD_OK;
@@ -292,27 +333,48 @@ extern "C" int aspd_workspace_init(void* workspace_d, size_t workspace_bytes, vo
 extern "C" int aspd_attn_parallel_decode(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
                                          const void* q_d, void* out_d, float* lse_d, float sm_scale,
                                          void* workspace_d, size_t workspace_bytes, void* stream) {
-  return attn_launch(MODE_PARALLEL, kv, state, step, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes,
+  return attn_launch(MODE_PARALLEL, kv, state, step, nullptr, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes,
                      stream);
+}
+
+extern "C" int aspd_attn_parallel_decode_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                  const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d, float sm_scale,
+                                  void* workspace_d, size_t workspace_bytes, void* stream) {
+  if (!scores) return ASPD_ERR_INVALID_ARG;
+  return attn_launch(MODE_PARALLEL, kv, state, step, scores, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes, stream);
 }
 
 extern "C" int aspd_attn_branch_chunk(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
                                       const void* q_d, void* out_d, float* lse_d, float sm_scale,
                                       void* workspace_d, size_t workspace_bytes, void* stream) {
-  return attn_launch(MODE_CHUNK, kv, state, step, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes,
+  return attn_launch(MODE_CHUNK, kv, state, step, nullptr, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes,
                      stream);
+}
+
+extern "C" int aspd_attn_branch_chunk_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                  const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d, float sm_scale,
+                                  void* workspace_d, size_t workspace_bytes, void* stream) {
+  if (!scores) return ASPD_ERR_INVALID_ARG;
+  return attn_launch(MODE_CHUNK, kv, state, step, scores, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes, stream);
 }
 
 extern "C" int aspd_attn_serial_decode(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
                                        const void* q_d, void* out_d, float* lse_d, float sm_scale,
                                        void* workspace_d, size_t workspace_bytes, void* stream) {
-  return attn_launch(MODE_SERIAL, kv, state, step, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes,
+  return attn_launch(MODE_SERIAL, kv, state, step, nullptr, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes,
                      stream);
 }
 
-extern "C" int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
-                                       const void* q_d, void* out_d, float* lse_d, float sm_scale,
-                                       void* workspace_d, size_t workspace_bytes, void* stream) {
+extern "C" int aspd_attn_serial_decode_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                  const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d, float sm_scale,
+                                  void* workspace_d, size_t workspace_bytes, void* stream) {
+  if (!scores) return ASPD_ERR_INVALID_ARG;
+  return attn_launch(MODE_SERIAL, kv, state, step, scores, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes, stream);
+}
+
+namespace {
+int sequence_launch(const aspd_kv* kv, const aspd_state* state, const aspd_step* step, const aspd_scores* scores, const void* q_d,
+                    void* out_d, float* lse_d, float sm_scale, void* workspace_d, size_t workspace_bytes, void* stream) {
   int rc = aspd_check_kv(kv);
   if (rc != ASPD_OK) return rc;
   if (!state || !step || state->B <= 0) return ASPD_ERR_INVALID_ARG;
@@ -328,6 +390,7 @@ extern "C" int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* stat
   if (!step->q_branch_d || !step->logical_slot_d || !q_d || !out_d) return ASPD_ERR_INVALID_ARG;
   if (((uintptr_t)q_d & 15) || ((uintptr_t)out_d & 15)) return ASPD_ERR_INVALID_ARG;
   if (!(sm_scale >= 0.f)) return ASPD_ERR_INVALID_ARG;
+  if (scores && (rc = check_scores(kv, state, step, scores)) != ASPD_OK) return rc;
   const bool branches = step->shared_mask == 0;
   if (branches && (!state->slot_owner_d || state->owner_stride < kv->max_blocks_per_seq * ASPD_BLOCK ||
                    (state->owner_stride & 3) || ((uintptr_t)state->slot_owner_d & 3)))
@@ -359,6 +422,7 @@ extern "C" int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* stat
   a.row_lo = step->plan_d + aspd_sequence_plan_lo(G, state->B, step->NQ);
   a.NQ = step->NQ;
   a.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)kv->head_dim) : sm_scale) * LOG2E;
+  set_scores(&a, state, step, scores);
   a.B = state->B;
   a.G = G;
   a.inv_G = 1.f / (float)G;
@@ -371,23 +435,43 @@ extern "C" int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* stat
   if (step->max_workgroups > 0) nwg = std::min(nwg, (long)step->max_workgroups);
   a.nwg = (int)std::max(1L, nwg);
   hipStream_t hs = (hipStream_t)stream;
-#define ASPD_SEQ_LAUNCH(DD, PIECES)                                                                                      \
-  do {                                                                                                                   \
-    rc = allow_big_lds((const void*)attn_bf16_seq_kernel<DD, ROWS_NW, PIECES>);                                          \
-    if (rc != ASPD_OK) return rc;                                                                                        \
-    hipLaunchKernelGGL((attn_bf16_seq_kernel<DD, ROWS_NW, PIECES>), dim3(a.nwg), dim3(ROWS_NW * 64), (rows_smem_bytes<DD>()), \
-                       hs, a);                                                                                           \
+#define ASPD_SEQ_KERNEL(DD, PIECES, CAP, BIAS)                                                                        \
+  do {                                                                                                               \
+    rc = allow_big_lds((const void*)attn_bf16_seq_kernel<DD, ROWS_NW, PIECES, CAP, BIAS>);                           \
+    if (rc != ASPD_OK) return rc;                                                                                    \
+    hipLaunchKernelGGL((attn_bf16_seq_kernel<DD, ROWS_NW, PIECES, CAP, BIAS>), dim3(a.nwg), dim3(ROWS_NW * 64),      \
+                       (rows_smem_bytes<DD, BIAS>()), hs, a);                                                        \
   } while (0)
-  if (kv->head_dim == 128) {
-    if (pieces) ASPD_SEQ_LAUNCH(128, true);
-    else ASPD_SEQ_LAUNCH(128, false);
-  } else {
-    if (pieces) ASPD_SEQ_LAUNCH(64, true);
-    else ASPD_SEQ_LAUNCH(64, false);
-  }
+#define ASPD_SEQ_LAUNCH(CAP, BIAS)                             \
+  do {                                                         \
+    if (kv->head_dim == 128) {                                 \
+      if (pieces) ASPD_SEQ_KERNEL(128, true, CAP, BIAS);       \
+      else ASPD_SEQ_KERNEL(128, false, CAP, BIAS);             \
+    } else {                                                   \
+      if (pieces) ASPD_SEQ_KERNEL(64, true, CAP, BIAS);        \
+      else ASPD_SEQ_KERNEL(64, false, CAP, BIAS);              \
+    }                                                          \
+  } while (0)
+  ASPD_CHANGED(ASPD_SEQ_LAUNCH);
 #undef ASPD_SEQ_LAUNCH
+#undef ASPD_SEQ_KERNEL
+#undef ASPD_CHANGED
   ASPD_HIP_CHECK(hipGetLastError());
   return ASPD_OK;
+}
+}  // namespace
+
+extern "C" int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                       const void* q_d, void* out_d, float* lse_d, float sm_scale,
+                                       void* workspace_d, size_t workspace_bytes, void* stream) {
+  return sequence_launch(kv, state, step, nullptr, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes, stream);
+}
+
+extern "C" int aspd_attn_full_sequence_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,
+                                              const aspd_scores* scores, const void* q_d, void* out_d, float* lse_d,
+                                              float sm_scale, void* workspace_d, size_t workspace_bytes, void* stream) {
+  if (!scores) return ASPD_ERR_INVALID_ARG;
+  return sequence_launch(kv, state, step, scores, q_d, out_d, lse_d, sm_scale, workspace_d, workspace_bytes, stream);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -424,6 +508,6 @@ extern "C" int aspd_attn_parallel_decode_static(const aspd_kv* kv, const aspd_st
   void* ws = nullptr;
   int rc = static_scratch(&ws);
   if (rc != ASPD_OK) return rc;
-  rc = attn_launch(MODE_PARALLEL, kv, state, step, q_d, out_d, lse_d, sm_scale, ws, ASPD_STATIC_SCRATCH_BYTES, stream);
+  rc = attn_launch(MODE_PARALLEL, kv, state, step, nullptr, q_d, out_d, lse_d, sm_scale, ws, ASPD_STATIC_SCRATCH_BYTES, stream);
   return rc == ASPD_ERR_WORKSPACE ? ASPD_ERR_SCRATCH_LIMIT : rc;
 }

@@ -13,6 +13,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/device_lazy_init.h>
@@ -30,7 +31,9 @@ PyObject *g_kv_type, *g_state_type, *g_step_type;  // the binding's classes (set
 // so that the calls here and those by ctypes are always calls of one.
 #define ASPD_CALLS(X)                                                                                                  \
   X(attn_parallel_decode) X(attn_branch_chunk) X(attn_serial_decode) X(attn_full_sequence)                             \
-  X(attn_parallel_decode_static) X(rope_append) X(build_branch_meta) X(sequence_plan_bytes) X(build_sequence_meta)
+  X(attn_parallel_decode_static) X(attn_parallel_decode_scored) X(attn_branch_chunk_scored)                            \
+  X(attn_serial_decode_scored) X(attn_full_sequence_scored) X(rope_append) X(norm_rope_append) X(build_branch_meta)    \
+  X(sequence_plan_bytes) X(build_sequence_meta)
 #define ASPD_POINTER(name) decltype(&aspd_##name) name;
 struct {
   ASPD_CALLS(ASPD_POINTER)
@@ -42,7 +45,9 @@ struct {
   X(k) X(v) X(block_tables) X(num_q_heads) X(B) X(NB) X(stage_base) X(seq_len) X(cu_branches) X(branch_len)            \
   X(slot_owner) X(owner_stride) X(fault) X(main_pos) X(stage_open) X(NQ) X(max_new_per_seq) X(max_workgroups)          \
   X(shared_mask) X(cu_new) X(cu_seq_new) X(q_seq) X(q_branch) X(position_ids) X(logical_slot) X(slot_mapping)          \
-  X(kv_len) X(plan) X(plan_key) X(pos_mode) X(data_ptr) X(numel) X(element_size) X(cuda_stream)
+  X(kv_len) X(plan) X(plan_key) X(pos_mode) X(data_ptr) X(numel) X(element_size) X(cuda_stream) X(rope_theta)          \
+  X(axis_of_pair) X(axis_pos) X(pos_offset) X(q_weight) X(k_weight) X(norm_eps) X(weight_offset) X(softcap) X(slopes)  \
+  X(slot_pos)
 #define ASPD_DECLARE(name) PyObject* n_##name;
 ASPD_NAMES(ASPD_DECLARE)
 PyObject* n_struct;
@@ -309,6 +314,182 @@ PyObject* py_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Arguments that bring a layout of their own are looked at before their addresses are taken: a ValueError names the first
+// that is not as the call needs it.
+struct Layouts {
+  const at::Tensor& cache;  // what the others have to lie beside
+  at::ScalarType type() const { return cache.scalar_type(); }
+
+  static bool refuse(const char* name, const char* what) {
+    PyErr_Format(PyExc_ValueError, "%s: %s", name, what);
+    return false;
+  }
+  // A tensor of that type beside the cache (None: null where it may be left out).
+  bool tensor(PyObject* o, const char* name, at::ScalarType type, bool optional, const at::Tensor** out) const {
+    *out = nullptr;
+    if (o == Py_None) return optional || refuse(name, "is missing");
+    if (!THPVariable_Check(o)) return refuse(name, "is no tensor");
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.layout() != at::kStrided) return refuse(name, "is not strided");
+    if (t.scalar_type() != type) return refuse(name, "has another type than the call takes");
+    if (t.device() != cache.device()) return refuse(name, "is not on the device of the cache");
+    *out = &t;
+    return true;
+  }
+  // [at least n] side by side.
+  bool row(PyObject* o, const char* name, at::ScalarType type, int64_t n, const void** out) const {
+    const at::Tensor* t;
+    *out = nullptr;
+    if (!tensor(o, name, type, true, &t)) return false;
+    if (!t) return true;
+    if (t->dim() != 1 || t->size(0) < n || (n > 1 && t->stride(0) != 1)) return refuse(name, "is not a row of the length the call needs");
+    *out = t->data_ptr();
+    return true;
+  }
+  // [at least n][heads][head_dim], heads and their elements side by side; stride 0: rows too.
+  bool heads(PyObject* o, const char* name, int64_t n, int64_t heads, int64_t dim, void** out, int64_t* stride) const {
+    const at::Tensor* t;
+    if (!tensor(o, name, type(), false, &t)) return false;
+    if (t->dim() != 3 || t->size(0) < n || t->size(1) != heads || t->size(2) != dim)
+      return refuse(name, "is not [rows][heads][head_dim] of the step and the cache");
+    if (t->stride(2) != 1 || (heads > 1 && t->stride(1) != dim)) return refuse(name, "has heads that do not lie side by side");
+    *stride = n > 1 ? t->stride(0) : 0;
+    if (n > 1 && *stride < heads * dim) return refuse(name, "has rows that overlap");
+    *out = t->data_ptr();
+    return true;
+  }
+  bool packed(PyObject* o, const char* name, int64_t n, int64_t heads_, int64_t dim, void** out) const {
+    int64_t stride;
+    return heads(o, name, n, heads_, dim, out, &stride) && (stride == 0 || stride == heads_ * dim || refuse(name, "is not packed"));
+  }
+  // [B][owner_stride] int32.
+  bool slots(PyObject* o, int64_t B, int64_t stride, void** out) const {
+    const at::Tensor* t;
+    *out = nullptr;
+    if (!tensor(o, "slot_pos", at::kInt, true, &t)) return false;
+    if (!t) return true;
+    if (t->dim() != 2 || t->size(0) < B || t->size(1) != stride || (B > 1 && t->stride(0) != stride) || t->stride(1) != 1)
+      return refuse("slot_pos", "is not [sequences][owner_stride] of the state");
+    *out = t->data_ptr();
+    return true;
+  }
+};
+
+// The cache's keys, on the device that is current (a launch elsewhere would get addresses of this one).
+const at::Tensor* cache_keys(Ref& k) {
+  if (!k.o) return nullptr;
+  if (!THPVariable_Check(k.o)) {
+    PyErr_SetString(PyExc_ValueError, "the cache's keys are no tensor");
+    return nullptr;
+  }
+  const at::Tensor& t = THPVariable_Unpack(k.o);
+  if (t.is_cuda() && t.get_device() != c10::hip::current_device()) {
+    PyErr_SetString(PyExc_ValueError, "the cache is not on the current device");
+    return nullptr;
+  }
+  return &t;
+}
+
+// (which, kv, state, step, q, out, lse, sm_scale, workspace, stream, scores) -> status
+PyObject* py_attn_scored(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    int32_t which;
+    aspd_kv kv;
+    aspd_state st;
+    aspd_step sp;
+    aspd_scores sc;
+    void *q, *out, *lse, *ws, *stream, *slot_pos;
+    size_t ws_bytes;
+    float scale;
+    if (!int_of(a[0], &which) || !fill(a[1], &kv) || !fill(a[2], &st) || !fill(a[3], &sp) || !bytes_of(a[8], &ws_bytes) ||
+        !address(a[6], &lse) || !float_of(a[7], &scale) || !address(a[8], &ws) || !stream_of(a[9], &stream))
+      return nullptr;
+    Ref k(PyObject_GetAttr(a[1], n_k)), cap(PyObject_GetAttr(a[10], n_softcap)), slopes(PyObject_GetAttr(a[10], n_slopes)),
+        pos(PyObject_GetAttr(a[10], n_slot_pos));
+    if (!cap.o || !slopes.o || !pos.o || !float_of(cap.o, &sc.softcap)) return nullptr;
+    const at::Tensor* keys = cache_keys(k);
+    if (!keys) return nullptr;
+    const Layouts of{*keys};
+    const void* slope;
+    if (!of.packed(a[4], "q", sp.NQ, kv.num_q_heads, kv.head_dim, &q) || !of.packed(a[5], "out", sp.NQ, kv.num_q_heads, kv.head_dim, &out) ||
+        !of.row(slopes.o, "slopes", at::kFloat, kv.num_q_heads, &slope) || !of.slots(pos.o, st.B, st.owner_stride, &slot_pos))
+      return nullptr;
+    sc.slopes_d = (const float*)slope;
+    sc.slot_pos_d = (const int32_t*)slot_pos;
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    switch (which) {
+      case PARALLEL: rc = g_lib.attn_parallel_decode_scored(&kv, &st, &sp, &sc, q, out, (float*)lse, scale, ws, ws_bytes, stream); break;
+      case CHUNK: rc = g_lib.attn_branch_chunk_scored(&kv, &st, &sp, &sc, q, out, (float*)lse, scale, ws, ws_bytes, stream); break;
+      case SERIAL: rc = g_lib.attn_serial_decode_scored(&kv, &st, &sp, &sc, q, out, (float*)lse, scale, ws, ws_bytes, stream); break;
+      default: rc = g_lib.attn_full_sequence_scored(&kv, &st, &sp, &sc, q, out, (float*)lse, scale, ws, ws_bytes, stream); break;
+    }
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+  });
+}
+
+// (kv, state, step, rotary, q, k_new, v_new, q_out, slot_pos, stream) -> status
+PyObject* py_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 10, [&]() -> PyObject* {
+    aspd_kv kv;
+    aspd_state st;
+    aspd_step sp;
+    aspd_rotary how;
+    void *q, *k, *v, *q_out = nullptr, *slot_pos, *stream;
+    int64_t qs, ks, vs;
+    if (!fill(a[0], &kv) || !fill(a[1], &st) || !fill(a[2], &sp) || !stream_of(a[9], &stream)) return nullptr;
+    Ref keys_of(PyObject_GetAttr(a[0], n_k));
+    const at::Tensor* keys = cache_keys(keys_of);
+    if (!keys) return nullptr;
+    const Layouts of{*keys};
+    const int64_t rows = sp.NQ;
+    if (!of.heads(a[4], "q", rows, kv.num_q_heads, kv.head_dim, &q, &qs) ||
+        !of.heads(a[5], "k_new", rows, kv.num_kv_heads, kv.head_dim, &k, &ks) ||
+        !of.heads(a[6], "v_new", rows, kv.num_kv_heads, kv.head_dim, &v, &vs) ||
+        !of.slots(a[8], st.B, st.owner_stride, &slot_pos))
+      return nullptr;
+    if (a[7] != Py_None && !of.packed(a[7], "q_out", rows, kv.num_q_heads, kv.head_dim, &q_out)) return nullptr;
+    Ref theta(PyObject_GetAttr(a[3], n_rope_theta)), of_pair(PyObject_GetAttr(a[3], n_axis_of_pair)),
+        axis_pos(PyObject_GetAttr(a[3], n_axis_pos)), offset(PyObject_GetAttr(a[3], n_pos_offset)),
+        qw(PyObject_GetAttr(a[3], n_q_weight)), kw(PyObject_GetAttr(a[3], n_k_weight)),
+        eps(PyObject_GetAttr(a[3], n_norm_eps)), add(PyObject_GetAttr(a[3], n_weight_offset));
+    if (!theta.o || !of_pair.o || !axis_pos.o || !offset.o || !qw.o || !kw.o || !eps.o || !add.o ||
+        !float_of(theta.o, &how.rope_theta) || !float_of(eps.o, &how.norm_eps) || !float_of(add.o, &how.weight_offset))
+      return nullptr;
+    const void *positions, *qw_at, *kw_at;
+    if (!of.row(offset.o, "pos_offset", at::kInt, st.B, &positions) ||
+        !of.row(qw.o, "q_weight", of.type(), kv.head_dim, &qw_at) || !of.row(kw.o, "k_weight", of.type(), kv.head_dim, &kw_at))
+      return nullptr;
+    how.pos_offset_d = (const int32_t*)positions;
+    how.q_weight_d = qw_at;
+    how.k_weight_d = kw_at;
+    const at::Tensor* axes;
+    if (!of.tensor(axis_pos.o, "axis_pos", at::kInt, true, &axes)) return nullptr;
+    if (axes && (axes->dim() != 2 || axes->size(1) < rows || axes->size(0) > INT32_MAX || (rows > 1 && axes->stride(1) != 1) ||
+                 (axes->size(0) > 1 && axes->stride(0) < rows))) {
+      PyErr_SetString(PyExc_ValueError, "axis_pos: is not [axes][rows] of the step");
+      return nullptr;
+    }
+    how.axis_pos_d = axes ? (const int32_t*)axes->data_ptr() : nullptr;
+    how.num_axes = axes ? (int32_t)axes->size(0) : 0;
+    how.axis_stride = axes ? (axes->size(0) > 1 ? axes->stride(0) : axes->size(1)) : 0;
+    how.axis_of_pair = nullptr;
+    if (of_pair.o != Py_None) {
+      if (!PyBytes_Check(of_pair.o) || PyBytes_GET_SIZE(of_pair.o) != kv.head_dim / 2) {
+        PyErr_SetString(PyExc_ValueError, "axis_of_pair: is not head_dim / 2 bytes");
+        return nullptr;
+      }
+      how.axis_of_pair = (const uint8_t*)PyBytes_AS_STRING(of_pair.o);
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = g_lib.norm_rope_append(&kv, &st, &sp, &how, q, qs, k, ks, v, vs, q_out, (int32_t*)slot_pos, stream);
+    Py_END_ALLOW_THREADS;
+    return PyLong_FromLong(rc);
+  });
+}
+
 // (kv, step, q, k_new, v_new, rope_theta, stream) -> status
 PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> PyObject* {
@@ -428,9 +609,9 @@ PyObject* py_init(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 #define ASPD_METHOD(name) {#name, (PyCFunction)(void (*)())py_##name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {ASPD_METHOD(attn), ASPD_METHOD(rope_append), ASPD_METHOD(build_branch_meta),
-                         ASPD_METHOD(sequence_plan_bytes), ASPD_METHOD(build_sequence_meta), ASPD_METHOD(structs),
-                         ASPD_METHOD(init), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {ASPD_METHOD(attn), ASPD_METHOD(attn_scored), ASPD_METHOD(rope_append), ASPD_METHOD(norm_rope_append),
+                         ASPD_METHOD(build_branch_meta), ASPD_METHOD(sequence_plan_bytes), ASPD_METHOD(build_sequence_meta),
+                         ASPD_METHOD(structs), ASPD_METHOD(init), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_pycalls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -30,7 +30,7 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
-template <int D>
+template <int D, bool BIAS = false>
 struct RowsCfg {
   static constexpr int CH = D / 8;          // 16-byte chunks per row
   static constexpr int PAGE_U4 = 16 * CH;
@@ -38,7 +38,8 @@ struct RowsCfg {
   static constexpr int MT = D / 32;         // 32-wide d-tiles of the value product
   static constexpr int PAGE_B = PAGE_U4 * 16;
   static constexpr int PAIR_B = 2 * PAGE_B;               // both pages of a pair: 32 consecutive rows
-  static constexpr int STAGE_B = 2 * ROWS_PPS * PAIR_B;   // K pairs, then V pairs
+  static constexpr int POS = 2 * ROWS_PPS * PAIR_B;       // K pairs, then V pairs, then with a bias by distance the positions
+  static constexpr int STAGE_B = POS + (BIAS ? 2 * ROWS_PPS * 256 : 0);  // of the K pages' keys (64 bytes, loaded 4 times over)
   // Pages lie in LDS as they do in the cache (they are loaded straight into it, 64 x 16 bytes in a row per
   // instruction), but for the order of the 16-byte chunks inside a row, which is chosen so that no read has a bank
   // conflict: a K operand read takes one chunk of sixteen rows at a time, a transposing V read 64 bytes of four.
@@ -52,8 +53,8 @@ struct RowsCfg {
 // 357, 12 of up to 1000 at 32/8 149 / 149 / 153; the 64-sequence chunk 1727 / 1739 / 1754; prompts 433 / 434 / 436.
 constexpr int ROWS_BUFS = 4;
 
-template <int D>
-constexpr size_t rows_smem_bytes() { return (size_t)ROWS_BUFS * RowsCfg<D>::STAGE_B; }
+template <int D, bool BIAS = false>
+constexpr size_t rows_smem_bytes() { return (size_t)ROWS_BUFS * RowsCfg<D, BIAS>::STAGE_B; }
 
 // One wave's 32 rows: lane (c, h) keeps the statistics of row c (its share of the sum) and O^T[32 mt + 8 b + 4 h +
 // j][c] in acc[mt][4 b + j].
@@ -135,10 +136,11 @@ struct Result {
   bool complete;
   float* pslot;
 };
-template <int D, int NW, bool SEQ, typename ResultOf>
+// CAP, BIAS: scores are changed (changed_score) as soon as a pair's are there; `scale` is in them then.
+template <int D, int NW, bool SEQ, bool CAP, bool BIAS, typename ResultOf>
 __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const Seg& it, ResultOf result,
                                             int* take_from) {
-  using C = RowsCfg<D>;
+  using C = RowsCfg<D, BIAS>;
   constexpr int PPS = ROWS_PPS;
   static_assert(PPS == 2 && NW == 4 * PPS, "one wave per page of a group");
   constexpr int LPT = C::PAGE_U4 / 64;      // 16-byte loads per lane and page
@@ -191,6 +193,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
     const int p = min(max(2 * i + l_pair + (l_is_k ? 1 : -1), 0), n_last);
     return min(page_of_pair(p) + (wave & 1), page1 - 1);
   };
+  const int32_t* const pos_row = BIAS ? a.slot_pos + (long)it.s * a.pos_stride : nullptr;
   const char* const pool = (const char*)(l_is_k ? a.kv.k : a.kv.v) + (long)it.h * C::PAGE_B;
   const uint32_t l_at = lds0 + (l_is_k ? 0 : PPS * C::PAIR_B) + l_pair * C::PAIR_B + (wave & 1) * C::PAGE_B;
   // Which 16 bytes of its page the lane fetches with the first load; with the k-th, 1024 k bytes on, and with the
@@ -217,7 +220,9 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   // opening over 12 sequences 59.6 -> 58.9, eight prompts 138.3 -> 137.3, three whole sequences 45.5 -> 45.1).
   __syncthreads();  // LDS of the previous segment is free
   bf16x8 qr[C::KSTEPS];
-  int slot, branch = 0, base = it.L, lo = 0;
+  int slot, branch = 0, base = it.L, lo = 0, q_pos = 0;
+  float slope = 0.f;
+  const float scale = CAP || BIAS ? 1.f : a.scale_log2;
   {
     const int rr = min(wave * 32 + c, R - 1);  // padding rows (and idle waves) repeat the last row
     const int qi = div_by_g(a, rr), q = it.q0 + qi;
@@ -229,6 +234,10 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       lo = a.slot_owner ? a.row_lo[q] : -1;
     } else {
       branch = a.q_branch[q];
+    }
+    if (BIAS) {
+      q_pos = a.position_ids[q];
+      slope = a.slopes[head] * LOG2E;
     }
     const u32x4* qsrc = (const u32x4*)a.q + ((long)q * a.kv.num_q_heads + head) * C::CH + h;
 #pragma unroll
@@ -246,6 +255,9 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
     const char* src = pool + (long)min(max(block, 0), a.kv.num_blocks - 1) * a.kv.num_kv_heads * C::PAGE_B;
 #pragma unroll
     for (int k = 0; k < LPT; ++k) load_to_lds(src + k * 1024, goff ^ (k * goff_flip), l_at + buffer_of(i) * C::STAGE_B + k * 1024);
+    if (BIAS && l_is_k)
+      load4_to_lds(pos_row + page_of_group(i) * ASPD_BLOCK, 4 * (lane & 15),
+                   lds0 + buffer_of(i) * C::STAGE_B + C::POS + (2 * l_pair + (wave & 1)) * 256);
   };
   auto clear_v = [&](int i, int k) {
     *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(l_at + buffer_of(i) * C::STAGE_B + k * 1024 + lane * 16) =
@@ -378,6 +390,20 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
 #pragma unroll
   for (int u = 0; u < PPS; ++u) tg[u][0] = tg[u][1] = u32x4{0, 0, 0, 0};
 
+  // Scores of the K pair in slot u of the current group, changed.  (va[0] of any lane lies behind the start of the stage by
+  // what it did in the first one.)
+  const uint32_t pa = BIAS ? lds0 + (ROWS_BUFS - 1) * C::STAGE_B + C::POS + 16 * h - va[0] : 0;
+  auto change = [&](int u, f32x16& s) {
+    if (!CAP && !BIAS) return;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      typedef int i32x4_lds __attribute__((ext_vector_type(4)));
+      i32x4_lds k_pos = {0, 0, 0, 0};
+      if (BIAS) k_pos = *(const __attribute__((address_space(3))) i32x4_lds*)(uintptr_t)(va[0] + pa + (2 * u + (b >> 1)) * 256 + 32 * (b & 1));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[4 * b + j] = changed_score<CAP, BIAS>(a, s[4 * b + j], slope, k_pos[j] - q_pos);
+    }
+  };
   // Step p (slot u of its group): scores of pair p + 1 (into `s_next`), value products of pair p - 1 (weights `p_prev`),
   // softmax of pair p.  In a full step all three take part.  Its order is written out, one slot per matrix
   // instruction, and held by the scheduling barriers: score and value products in turn (neighbours never wait for each
@@ -404,7 +430,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   auto step_full = [&](int u, bool ahead, const f32x16& s_cur, f32x16& s_next, const bf16x8 (&p_prev)[2], bf16x8 (&p_cur)[2]) {
     constexpr int PER = 16 / (2 * NP);  // weights per slot
     float sum[2] = {0.f, 0.f}, x[PER], w_last = 0.f;
-    auto exponent = [&](int i) { return fmaf(s_cur[i], a.scale_log2, rs.neg_ref); };
+    auto exponent = [&](int i) { return fmaf(s_cur[i], scale, rs.neg_ref); };
     auto weights = [&](int slot_index) {
 #pragma unroll
       for (int e = 0; e < PER; ++e) {
@@ -436,6 +462,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       weights(2 * j + 1);
       __builtin_amdgcn_sched_barrier(0);
     }
+    change(u, s_next);
     return sum[0] + sum[1] + w_last;
   };
   // The same for pairs that need a mask or are not seen at all, one part after the other.
@@ -471,8 +498,8 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
           s_cur[i] = vis ? s_cur[i] : -INFINITY;
         }
       }
-      float sum = rows_weights<D>(s_cur, rs, p_cur, a.scale_log2);
-      if (__any(sum > rs.limit)) sum = rows_raise<D>(s_cur, rs, p_cur, a.scale_log2);
+      float sum = rows_weights<D>(s_cur, rs, p_cur, scale);
+      if (__any(sum > rs.limit)) sum = rows_raise<D>(s_cur, rs, p_cur, scale);
       rs.l_run += sum;
     }
     if (see_next) {
@@ -484,6 +511,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
         if (j + RK < NP) kf[j % RK] = k_operand(u, j + RK);
         __builtin_amdgcn_sched_barrier(0);
       }
+      change(u, s_next);
     }
     see_prev = see;
     see = see_next;
@@ -496,8 +524,12 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   // hold anything, or an infinity that belongs to another slot, and zero times either would be a NaN.
   const int v_last = min(last_slot, page1 * ASPD_BLOCK - 1);
   auto arrive = [&](int i, bool tail) {
-    if (i + 1 <= i_last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LPT) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (i + 1 <= i_last) {
+      if (BIAS && l_is_k) wait_loads<LPT + 1>();
+      else wait_loads<LPT>();
+    } else {
+      wait_loads<0>();
+    }
     if (tail && !l_is_k) {
       const int key0 = (page_of_pair(2 * i - 1 + l_pair) + (wave & 1)) * ASPD_BLOCK;
       if (key0 + ASPD_BLOCK > v_last + 1) {
@@ -537,10 +569,10 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       arrive(i, false);
       fetch_first(0);
       float sum = step_full(0, true, s0, s1, p1, p0);
-      if (__any(sum > rs.limit)) sum = rows_raise<D>(s0, rs, p0, a.scale_log2);
+      if (__any(sum > rs.limit)) sum = rows_raise<D>(s0, rs, p0, scale);
       rs.l_run += sum;
       sum = step_full(1, false, s1, s0, p0, p1);
-      if (__any(sum > rs.limit)) sum = rows_raise<D>(s1, rs, p1, a.scale_log2);
+      if (__any(sum > rs.limit)) sum = rows_raise<D>(s1, rs, p1, scale);
       rs.l_run += sum;
       next_group(i);
     }
@@ -640,7 +672,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   return taken;
 }
 
-template <int D, int NW>
+template <int D, int NW, bool CAP = false, bool BIAS = false>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4, NW / 4))) void attn_bf16_rows_kernel(
     AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -656,7 +688,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4,
   for (int i = 1; nseg > 0;) {
     const bool complete = seg_complete(seg);
     float* pslot = partial_slot(a, blockIdx.x, seg.page0 == 0 ? 1 : 0, D);
-    const int taken = segment_rows<D, NW, false>(a, smem, seg, [=]() -> Result { return {complete, pslot}; },
+    const int taken = segment_rows<D, NW, false, CAP, BIAS>(a, smem, seg, [=]() -> Result { return {complete, pslot}; },
                                                   queue > 0 ? a.counters + QUEUE_NEXT : nullptr);
     if (!complete && !a.merge_apart) announce_partial<D, true, THREADS, D / 16, 4>(a, seg, &merge_flag);
     int at;
@@ -697,7 +729,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4,
 // merges, as in the row-splitting kernel.  PIECES: there may be such a list, and there is room for partial results;
 // otherwise every group is taken whole.
 // ---------------------------------------------------------------------------------------------
-template <int D, int NW, bool PIECES>
+template <int D, int NW, bool PIECES, bool CAP = false, bool BIAS = false>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4, NW / 4))) void attn_bf16_seq_kernel(
     AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -819,7 +851,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(NW / 4,
       held[3] = seg.q0;
       held[4] = seg.nq | (seg.h << 16);
     }
-    taken = segment_rows<D, NW, true>(a, smem, seg, [&]() -> Result {
+    taken = segment_rows<D, NW, true, CAP, BIAS>(a, smem, seg, [&]() -> Result {
       if (!PIECES) return {true, nullptr};
       const int slot = __builtin_amdgcn_readfirstlane(held[0]);
       return {slot < 0, a.partial + (long)slot * a.rows_cap * (D + 4)};

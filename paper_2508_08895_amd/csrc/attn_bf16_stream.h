@@ -25,14 +25,16 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr int BLK_WIN = 512;   // pages of a segment whose block ids are in LDS at once
 
-template <int D, int NT>
+// BIAS: scores are biased by distance: positions of the keys, of the queries and the heads' slopes.
+template <int D, int NT, bool BIAS = false>
 struct StreamLds {
   static constexpr int NW = STREAM_NW;
   static constexpr int CH = D / 8;                        // 16-byte chunks per row
   static constexpr int PAGE_B = ASPD_BLOCK * D * 2;
   static constexpr int LPP = PAGE_B / 1024;               // loads per page
-  static constexpr int STAGE_B = 2 * PAGE_B + 256;        // K page, V page, owner tags (16 bytes, loaded 16 times over)
-  static constexpr int LOADS = 2 * LPP + 1;               // loads of a stage
+  static constexpr int POS = 2 * PAGE_B + 256;            // of a stage: the keys' positions (64 bytes, loaded 4 times over)
+  static constexpr int STAGE_B = POS + (BIAS ? 256 : 0);  // K page, V page, owner tags (16 bytes, loaded 16 times over)
+  static constexpr int LOADS = 2 * LPP + 1 + BIAS;        // loads of a stage
   static constexpr int WAVE_B = 2 * STAGE_B;              // two stages, or the accumulators of two tiles
   static constexpr int RED_ROW = D + 4;                   // floats per row there (the 16 rows a wave writes at once fall
                                                           // on different banks)
@@ -41,7 +43,8 @@ struct StreamLds {
   static constexpr int BLK = Q + NT * PAGE_B;             // [BLK_WIN] block ids of the window
   static constexpr int SLOT = BLK + BLK_WIN * 4;          // [64] logical slots of the row group's queries
   static constexpr int BRANCH = SLOT + 256;               // [64] their branches
-  static constexpr int M = BRANCH + 256;                  // [16 NT][NW] references of the waves
+  static constexpr int QPOS = BRANCH + 256;               // [64] their positions, [64] slopes of the heads
+  static constexpr int M = QPOS + (BIAS ? 512 : 0);       // [16 NT][NW] references of the waves
   static constexpr int L = M + 16 * NT * NW * 4;          // [16 NT][NW] sums
   static constexpr int TAKE = L + 16 * NT * NW * 4;       // [64] next page nobody has taken (word 0; see take())
   // (more than half of a compute unit's LDS: one workgroup per compute unit, as the grid is sized for)
@@ -58,11 +61,11 @@ struct StreamLds {
 // references raised at a score 2^6 above (as with pairs of pages), for queries ~ N(0, 1), N(0, 4) and N(0, 36).
 constexpr float STREAM_SUM_MAX = 20.f;
 
-template <int D, int NT, bool STREAM>
+template <int D, int NT, bool STREAM, bool CAP, bool BIAS>
 __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, const Seg& it, bool complete, float* pslot,
                                                int id0, int id1 /* blocks of the wave's first two pages, or what was
                                                thought to be: compared with the block table before the pages count */) {
-  using C = StreamLds<D, NT>;
+  using C = StreamLds<D, NT, BIAS>;
   constexpr int NW = C::NW, THREADS = NW * 64;
   constexpr int KSTEPS = D / 32, MT = D / 16, CH = C::CH;
   const int tid = threadIdx.x;
@@ -101,8 +104,11 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
     }
     if (wave == NW - 1) load4_to_lds(a.logical_slot + it.q0, 4 * min(lane, it.nq - 1), lds0 + C::SLOT);
     if (wave == NW - 2) load4_to_lds(a.q_branch + it.q0, 4 * min(lane, it.nq - 1), lds0 + C::BRANCH);
+    if (BIAS && wave == NW - 3) load4_to_lds(a.position_ids + it.q0, 4 * min(lane, it.nq - 1), lds0 + C::QPOS);
+    if (BIAS && wave == NW - 4) load4_to_lds(a.slopes + it.h * a.G, 4 * min(lane, a.G - 1), lds0 + C::QPOS + 256);
     load4_to_lds(bt, 4 * min(tid, np - 1), lds0 + C::BLK + wave * 256);
   }
+  const int32_t* const pos_row = BIAS ? a.slot_pos + (long)it.s * a.pos_stride + (long)page0 * ASPD_BLOCK : nullptr;
   const char* const own_row = a.slot_owner ? (const char*)(a.slot_owner + (long)it.s * a.owner_stride)
                                            : (const char*)a.logical_slot;  // (no tags: four bytes nobody looks at)
   const uint32_t own_off = a.slot_owner ? 4 * (lane & 3) : 0;
@@ -113,6 +119,7 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
     page_to_lds<D, STREAM>((const char*)a.kv.k + from, koff, at);
     page_to_lds<D, STREAM>((const char*)a.kv.v + from, voff, at + C::PAGE_B);
     load4_to_lds(own_row + (long)(page0 + page) * own_step, own_off, at + 2 * C::PAGE_B);
+    if (BIAS) load4_to_lds(pos_row + (long)page * ASPD_BLOCK, 4 * (lane & 15), at + C::POS);
   };
   int cur = wave, nxt = wave + NW;  // pages are numbered from the segment's first; past the end: none
   if (cur < np) issue(cur, id0, stage0);
@@ -149,9 +156,14 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
   constexpr bool Q_HELD = NT * D <= 256;  // in registers (more of them would spill)
   bf16x8 qf[NT][KSTEPS];
   const uint32_t q_back = lds0 + C::Q - stage0;
-  int slot[NT], tag[NT];
+  int slot[NT], tag[NT], q_pos[NT];
+  float slope[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
+    if (BIAS) {
+      q_pos[n] = lds_int(lds0 + C::QPOS + 4 * query[n]);
+      slope[n] = __builtin_bit_cast(float, lds_int(lds0 + C::QPOS + 256 + 4 * (min(16 * n + c, R - 1) - query[n] * a.G))) * LOG2E;
+    }
 #pragma unroll
     for (int t = 0; t < KSTEPS; ++t)
       if (Q_HELD) qf[n][t] = lds_operand(lds0 + C::Q + n * C::PAGE_B + ka[t]);
@@ -181,6 +193,7 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
   };
   auto block_of = [&](int page, int wpages) -> int { return lds_int(lds0 + C::BLK + 4 * min(page, wpages - 1)); };
 
+  const float scale = CAP || BIAS ? 1.f : a.scale_log2;  // (changed scores have it in them)
   // One page, from stage S of the wave.
   auto compute = [&](auto S, int page) {
     constexpr uint32_t at = decltype(S)::value * C::STAGE_B;
@@ -216,6 +229,16 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
     for (int t = 0; t < KSTEPS; ++t)
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t], qf[n][t], s[n], 0, 0, 0);
+    if (CAP || BIAS) {
+      typedef int i32x4_lds __attribute__((ext_vector_type(4)));
+      i32x4_lds k_pos = {0, 0, 0, 0};
+      if (BIAS) k_pos = *(const __attribute__((address_space(3))) i32x4_lds*)(uintptr_t)(stage0 + at + C::POS + 16 * g);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s[n][e] = changed_score<CAP, BIAS>(a, s[n][e], BIAS ? slope[n] : 0.f, BIAS ? k_pos[e] - q_pos[n] : 0);
+    }
     if (k_first + ASPD_BLOCK > mask_from) {  // (only pages that reach into the branch region or past a row's slot)
       const uint32_t own = (uint32_t)lds_int(stage0 + at + 2 * C::PAGE_B + 4 * g);
       const int k0 = k_first + 4 * g;
@@ -244,7 +267,7 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
         bf16x4 w4;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float w = __builtin_amdgcn_exp2f(fmaf(s[n][e], a.scale_log2, neg_ref[n]));
+          const float w = __builtin_amdgcn_exp2f(fmaf(s[n][e], scale, neg_ref[n]));
           sum += w;
           w4[e] = (__bf16)w;
         }
@@ -254,7 +277,7 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
       float sum = weights();
       if (__any(sum > limit[n])) {
         float mx = fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3]));
-        mx = over_quarters(mx, [](float x, float y) { return fmaxf(x, y); }) * a.scale_log2;  // scale > 0
+        mx = over_quarters(mx, [](float x, float y) { return fmaxf(x, y); }) * scale;  // scale > 0
         const float m_new = fmaxf(m_run[n], mx);
         const float ref = exp2_safe_ref(m_new);
         const float alpha = __builtin_amdgcn_exp2f(m_run[n] - ref);
@@ -390,7 +413,7 @@ __device__ __forceinline__ void segment_stream(const AttnArgs& a, char* smem, co
   }
 }
 
-template <int D, int NT, bool STREAM>
+template <int D, int NT, bool STREAM, bool CAP = false, bool BIAS = false>
 __global__ __launch_bounds__(STREAM_NW * 64) __attribute__((amdgpu_waves_per_eu(STREAM_NW / 4, STREAM_NW / 4))) void
 attn_bf16_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -414,7 +437,7 @@ attn_bf16_kernel(AttnArgs a) {
     if (i + 1 < nseg) after = plan_segment(a, next + i);
     const bool complete = seg_complete(seg);
     float* pslot = partial_slot(a, blockIdx.x, seg.page0 == 0 ? 1 : 0, D);
-    segment_stream<D, NT, STREAM>(a, smem, seg, complete, pslot, id0, id1);
+    segment_stream<D, NT, STREAM, CAP, BIAS>(a, smem, seg, complete, pslot, id0, id1);
     if (!complete) announce_partial<D, true, NW * 64, MERGE, (MERGE == 4 ? 6 : 16 / MERGE)>(a, seg, &merge_flag);
     if (++i >= nseg) break;
     seg = after;

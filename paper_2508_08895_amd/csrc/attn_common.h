@@ -51,7 +51,25 @@ struct AttnArgs {
   const int32_t* pieces;        // ... their list of pieces, and how many pieces `partial` (null: none) has slots for
   int            parts;
   int            merge_apart;   // row-splitting launches: partial results are left for a launch of their own
+  // launches on changed scores (aspd_scores), see changed_score
+  float          cap_in, cap_log2;       // 2 sm_scale log2(e) / softcap and softcap log2(e); 0: no cap
+  const float*   slopes;                 // null: no bias by distance
+  const int32_t* slot_pos;
+  int            pos_stride;
+  const int32_t* position_ids;
 };
+
+// A changed score in the log2 domain, sm_scale and log2(e) in it: from the product q.k, the row's slope (times log2(e)) and
+// the key's distance.  c tanh(s / c) = c - 2 c / (exp(2 s / c) + 1): where exp overflows it is c, where it vanishes -c.
+// Fewest instructions (two of them on the slow path of the vector unit); the subtraction leaves an error of 2^-23 c, hence the
+// bound on c: 2^-13 at c = 2^10, a fifth of what the weights' rounding to bf16 is.
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ float changed_score(const AttnArgs& a, float s, float slope_log2, int distance) {
+  float x = CAP ? fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * a.cap_in) + 1.f), a.cap_log2)
+                : s * a.scale_log2;
+  if (BIAS) x = fmaf(slope_log2, (float)distance, x);
+  return x;
+}
 
 // r / G for a row of a row group.  Exact: (r + 1/2) / G is at least 1 / (2 G) away from a whole number, and r < 768.
 // (An integer division by a value the compiler does not know is forty instructions, and with few waves on a SIMD every

@@ -34,7 +34,7 @@ __device__ __forceinline__ void halve(float* v, bool upper) {
   }
 }
 
-template <int D>
+template <int D, bool CHANGED>
 __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool complete, float* pslot) {
   constexpr int QD = D / 4;        // floats per lane per key
   constexpr int OWN = QD / 16;     // ... and of a row's combined output
@@ -50,7 +50,9 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
   float* qtile = (float*)smem;                           // [F32_ROWS][D]
   int* rowslot = (int*)(qtile + F32_ROWS * D);
   int* rowtag = rowslot + F32_ROWS;
-  float* part = (float*)(rowtag + F32_ROWS);             // [NW][F32_ROWS][D] sums of the waves
+  int* rowpos = rowtag + F32_ROWS;                       // of changed scores: positions and slopes of the rows
+  float* rowslope = (float*)(rowpos + (CHANGED ? F32_ROWS : 0));
+  float* part = rowslope + (CHANGED ? F32_ROWS : 0);     // [NW][F32_ROWS][D] sums of the waves
   float* stat = part + NW * F32_ROWS * D;                // [NW][F32_ROWS][2] reference, sum of the weights
 
   const int32_t* bt = a.kv.block_tables + (long)it.s * a.kv.max_blocks_per_seq;
@@ -60,6 +62,7 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
     float k[QD], v[QD];
     int own;
   };
+  const int32_t* pos_row = CHANGED && a.slopes ? a.slot_pos + (long)it.s * a.pos_stride : nullptr;
   auto fetch = [&](int P, int blk, Page& pg) {
     blk = min(max(blk, 0), a.kv.num_blocks - 1);
     const long off = (((long)blk * a.kv.num_kv_heads + it.h) * ASPD_BLOCK + k) * D + g * QD;
@@ -72,6 +75,10 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
     }
     const int j = min(P, page1 - 1) * ASPD_BLOCK + k;
     pg.own = (owner_row && j >= L && j < a.owner_stride) ? owner_row[j] : 0;
+  };
+  auto key_pos = [&](int P) -> int {  // position of the lane's key
+    const int j = min(P, page1 - 1) * ASPD_BLOCK + k;
+    return pos_row && j < a.pos_stride ? pos_row[j] : 0;
   };
   const int P0 = page0 + wave;
   int blk = block_of(P0), blk_next = block_of(P0 + NW);
@@ -89,6 +96,11 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
     rowslot[tid] = a.logical_slot[q];
     const int qb = a.q_branch[q];
     rowtag[tid] = (qb < 0 || !a.cu_branches) ? 0 : qb - a.cu_branches[it.s] + 1;
+    if (CHANGED) {
+      const int r = min(tid, R - 1);
+      rowpos[tid] = pos_row ? a.position_ids[q] : 0;
+      rowslope[tid] = pos_row ? a.slopes[it.h * a.G + r - div_by_g(a, r) * a.G] * LOG2E : 0.f;
+    }
   }
   Page cur, next;
   if (AHEAD) fetch(P0, blk, cur);
@@ -113,6 +125,7 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
     // D / 4 values per lane) they would not fit beside the accumulators.
     asm volatile("" ::: "memory");
     const int blk_after = block_of(P + 2 * NW);
+    const int at = CHANGED ? key_pos(P) : 0;
     if (AHEAD) fetch(P + NW, blk_next, next);
     else fetch(P, blk, cur);
     const int j = P * ASPD_BLOCK + k;
@@ -127,7 +140,13 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
       for (int e = 0; e < QD; ++e) s = fmaf(qtile[r * D + g * QD + e], cur.k[e], s);
       s += __shfl_xor(s, 16);
       s += __shfl_xor(s, 32);
-      s *= a.scale_log2;
+      if (CHANGED) {
+        // (the library's tanh here: nothing is lost for small scores, and what bounds this kernel is latency)
+        s = a.cap_log2 > 0.f ? a.cap_log2 * tanhf(0.5f * LN2 * a.cap_in * s) : s * a.scale_log2;
+        s = fmaf(rowslope[r], (float)(at - rowpos[r]), s);
+      } else {
+        s *= a.scale_log2;
+      }
       const bool vis = (j <= rowslot[r]) && (j < L || rowtag[r] == 0 || cur.own == rowtag[r]);
       // No branch on vis (an invisible key enters with weight zero): the lanes of one key agree on vis
       // and on s, so their statistics stay identical, and the whole update runs with all lanes active.
@@ -208,13 +227,13 @@ __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool c
   }
 }
 
-template <int D>
+template <int D, bool CHANGED = false>
 constexpr size_t f32_smem_bytes() {
-  return (F32_ROWS * D + 2 * F32_ROWS + NW * F32_ROWS * (D + 2)) * 4;
+  return (F32_ROWS * D + (CHANGED ? 4 : 2) * F32_ROWS + NW * F32_ROWS * (D + 2)) * 4;
 }
 
 // One workgroup per compute unit, one wave per SIMD, which may have all of its registers; the grid is sized for that.
-template <int D>
+template <int D, bool CHANGED = false>
 __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(1, 1))) void attn_f32_kernel(AttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int merge_flag;
@@ -228,7 +247,7 @@ __global__ __launch_bounds__(THREADS) __attribute__((amdgpu_waves_per_eu(1, 1)))
     }
     const bool complete = seg_complete(seg);
     float* pslot = partial_slot(a, blockIdx.x, seg.page0 == 0 ? 1 : 0, D);
-    segment_f32<D>(a, smem, seg, complete, pslot);
+    segment_f32<D, CHANGED>(a, smem, seg, complete, pslot);
     if (!complete) announce_partial<D, false, THREADS, 1, 16>(a, seg, &merge_flag);
   }
 }
