@@ -22,8 +22,8 @@ from .attention import _rows_f64
 def attend_scored(table, meta, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, softcap: float = 0.0,
                   slopes=None, scale: float | None = None, rows=None, shared_mask: bool = False, score_error=None):
     """Returns a dict of float64 arrays over the packed rows (NaN for rows not asked for): out [NQ][Hq][D], lse [NQ][Hq];
-    mass = sum_j p_j |v_j| [NQ][Hq][D]; keys [NQ] the keys a row sees; with score_error(s_abs, s, bias), the error of a score
-    whose products' absolute values sum to s_abs: error_mass = sum_j p_j e_j |v_j| and error = sum_j p_j e_j."""
+    mass = sum_j p_j |v_j| [NQ][Hq][D]; keys [NQ] the keys a row sees; with score_error(s_abs, s, bias, spread), the error of a
+    score whose products' absolute values sum to s_abs, spread being |slope| times the range of the rows' positions: error_mass = sum_j p_j e_j |v_j| and error = sum_j p_j e_j."""
     NQ, Hq, D = q.shape
     Hkv = k_cache.shape[1]
     G = Hq // Hkv
@@ -56,7 +56,8 @@ def attend_scored(table, meta, q: torch.Tensor, k_cache: torch.Tensor, v_cache: 
             got["lse"][idx, h] = (m + np.log(l))[:, 0]
             got["mass"][idx, h] = p @ np.abs(v)
             if score_error is not None:
-                e = p * score_error(np.abs(qf[idx, h]) @ np.abs(k).T * scale, np.where(mask, x - bias, 0.0), np.where(mask, bias, 0.0))
+                e = p * score_error(np.abs(qf[idx, h]) @ np.abs(k).T * scale, np.where(mask, x - bias, 0.0), np.where(mask, bias, 0.0),
+                                    0.0 if slopes is None else abs(float(slopes[h])) * (pos[slots].max() - pos[slots].min()))
                 got["error_mass"][idx, h] = e @ np.abs(v)
                 got["error"][idx, h] = e.sum(1)
     return got

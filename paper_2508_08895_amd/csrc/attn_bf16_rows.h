@@ -222,7 +222,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   bf16x8 qr[C::KSTEPS];
   int slot, branch = 0, base = it.L, lo = 0, q_pos = 0;
   float slope = 0.f;
-  const float scale = CAP || BIAS ? 1.f : a.scale_log2;
+  const float scale = CAP ? 1.f : a.scale_log2;  // (capped scores have it in them)
   {
     const int rr = min(wave * 32 + c, R - 1);  // padding rows (and idle waves) repeat the last row
     const int qi = div_by_g(a, rr), q = it.q0 + qi;
@@ -237,7 +237,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
     }
     if (BIAS) {
       q_pos = a.position_ids[q];
-      slope = a.slopes[head] * LOG2E;
+      slope = a.slopes[head] * (CAP ? LOG2E : LOG2E / a.scale_log2);  // (added to capped scores, or to products q.k)
     }
     const u32x4* qsrc = (const u32x4*)a.q + ((long)q * a.kv.num_q_heads + head) * C::CH + h;
 #pragma unroll
@@ -390,19 +390,57 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
 #pragma unroll
   for (int u = 0; u < PPS; ++u) tg[u][0] = tg[u][1] = u32x4{0, 0, 0, 0};
 
-  // Scores of the K pair in slot u of the current group, changed.  (va[0] of any lane lies behind the start of the stage by
-  // what it did in the first one.)
-  const uint32_t pa = BIAS ? lds0 + (ROWS_BUFS - 1) * C::STAGE_B + C::POS + 16 * h - va[0] : 0;
-  auto change = [&](int u, f32x16& s) {
-    if (!CAP && !BIAS) return;
+  // ---- changed scores.
+  // The cap alone is worked out with the weights: 2 c / (exp(2 s / c) + 1) two slots ahead of them, its constant beside the
+  // running reference.
+  // The bias is one more matrix product: of the keys' distances from `base` (the last row's position; 24 bits in three parts
+  // of eight, which bf16 holds exactly) with the slopes (three parts likewise) and of ones with slope * (base - the row's
+  // position), sixteen k-slots in all.  With a cap its result is added to the capped scores, which are written in place;
+  // without one to the products q.k, the slopes divided by sm_scale.  (A subtraction, a conversion and a product-sum for every
+  // score instead: the 64-token chunk 459 us for 312 without a bias, whole sequences 1 561 for 1 193.)
+  auto cap_part = [&](float x) -> float { return __builtin_amdgcn_exp2f(x * a.cap_in); };
+  auto capped = [&](float part, float constant) -> float {
+    return fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(part + 1.f), constant);
+  };
+  struct Parts {
+    float x[3];
+  };
+  auto parts_of = [](float x) -> Parts {
+    auto top = [](float v) { return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xffff0000u); };
+    Parts p;
+    p.x[0] = top(x);
+    p.x[1] = top(x - p.x[0]);
+    p.x[2] = x - p.x[0] - p.x[1];
+    return p;
+  };
+  const int base_pos = BIAS ? of_lane(q_pos, 31) : 0;
+  bf16x8 slopes;
+  if constexpr (BIAS) {
+    const Parts s = parts_of(slope), r = parts_of(slope * (float)(base_pos - q_pos));
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      typedef int i32x4_lds __attribute__((ext_vector_type(4)));
-      i32x4_lds k_pos = {0, 0, 0, 0};
-      if (BIAS) k_pos = *(const __attribute__((address_space(3))) i32x4_lds*)(uintptr_t)(va[0] + pa + (2 * u + (b >> 1)) * 256 + 32 * (b & 1));
+    for (int k = 0; k < 6; ++k) slopes[k] = (__bf16)s.x[k % 3];
+    slopes[6] = (__bf16)(h ? r.x[2] : r.x[0]);
+    slopes[7] = (__bf16)(h ? 0.f : r.x[1]);
+  }
+  // Position of key lane % 32 of the K pair in slot u of the current group.  (va[0] of any lane lies behind the start of the
+  // stage by what it did in the first one.)
+  const uint32_t pa = BIAS ? lds0 + (ROWS_BUFS - 1) * C::STAGE_B + C::POS + ((lane >> 4) & 1) * 256 + 4 * (lane & 15) - va[0] : 0;
+  auto position_of_key = [&](int u) -> int { return *(const __attribute__((address_space(3))) int*)(uintptr_t)(va[0] + pa + 2 * u * 256); };
+  auto keys_of = [&](int position) -> bf16x8 {
+    const Parts p = parts_of((float)(position - base_pos));
+    const float first = h ? p.x[2] : p.x[0], second = h ? 0.f : p.x[1];
+    bf16x8 keys;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[4 * b + j] = changed_score<CAP, BIAS>(a, s[4 * b + j], slope, k_pos[j] - q_pos);
-    }
+    for (int k = 0; k < 6; ++k) keys[k] = (__bf16)(k < 3 ? first : second);
+    keys[6] = keys[7] = (__bf16)1.f;
+    return keys;
+  };
+  auto add_bias = [&](bf16x8 keys, f32x16& s) { s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys, slopes, s, 0, 0, 0); };
+  int position = 0;  // of key lane % 32 of the pair whose weights are next (cap and bias)
+  auto finish = [&](f32x16& s) {  // scores with a cap as they will be, in the log2 domain
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = capped(cap_part(s[i]), a.cap_log2);
+    if constexpr (BIAS) add_bias(keys_of(position), s);
   };
   // Step p (slot u of its group): scores of pair p + 1 (into `s_next`), value products of pair p - 1 (weights `p_prev`),
   // softmax of pair p.  In a full step all three take part.  Its order is written out, one slot per matrix
@@ -427,16 +465,42 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   // (left to itself the compiler puts all sixteen, one waiting for the other, behind the last product).  Three whole
   // sequences 129.8 -> 126.7 us, 64-sequence chunk 1 438 -> 1 426, eight prompts 375.6 -> 371.7, 64 whole sequences 23.9 ->
   // 23.7 ms.
-  auto step_full = [&](int u, bool ahead, const f32x16& s_cur, f32x16& s_next, const bf16x8 (&p_prev)[2], bf16x8 (&p_cur)[2]) {
+  auto step_full = [&](int u, bool ahead, f32x16& s_cur, f32x16& s_next, const bf16x8 (&p_prev)[2], bf16x8 (&p_cur)[2]) {
     constexpr int PER = 16 / (2 * NP);  // weights per slot
-    float sum[2] = {0.f, 0.f}, x[PER], w_last = 0.f;
-    auto exponent = [&](int i) { return fmaf(s_cur[i], scale, rs.neg_ref); };
+    float sum[2] = {0.f, 0.f}, x[2 * PER], part[PER], w_last = 0.f;
+    int next_position = 0;
+    bf16x8 keys;
+    if constexpr (BIAS) next_position = position_of_key(u);
+    float constant = rs.neg_ref;
+    if constexpr (CAP && !BIAS) constant += a.cap_log2;
+    auto exponent = [&](int i, int e) {
+      if constexpr (!CAP) return fmaf(s_cur[i], a.scale_log2, rs.neg_ref);
+      else if constexpr (!BIAS) return capped(part[e], constant);
+      else return s_cur[i] + constant;
+    };
+    // with cap and bias: the caps in the first half of the slots, the weights in the second
+    constexpr int FIRST = CAP && BIAS ? NP : 0, PACE = CAP && BIAS ? 2 * PER : PER;
     auto weights = [&](int slot_index) {
+      if constexpr (CAP && BIAS) {
+        if (slot_index < FIRST) {
 #pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        const int i = slot_index * PER + e;
+          for (int e = 0; e < PACE; ++e) s_cur[slot_index * PACE + e] = capped(cap_part(s_cur[slot_index * PACE + e]), a.cap_log2);
+          if (slot_index == FIRST - 1) {
+            add_bias(keys, s_cur);
+#pragma unroll
+            for (int e = 0; e < PACE; ++e) x[e] = exponent(e, e);
+          }
+          return;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < PACE; ++e) {
+        const int i = (slot_index - FIRST) * PACE + e;
         const float w = __builtin_amdgcn_exp2f(x[e]);
-        if (i + PER < 16) x[e] = exponent(i + PER);
+        if (i + PACE < 16) x[e] = exponent(i + PACE, e);
+        if constexpr (CAP && !BIAS) {
+          if (i + 2 * PACE < 16) part[e] = cap_part(s_cur[i + 2 * PACE]);
+        }
         p_cur[i >> 3][i & 7] = (__bf16)w;
         if (i > 0) {
           sum[i & 1] += w_last;
@@ -447,13 +511,23 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
         if ((i & 7) == 7) asm volatile("" : "+v"(p_cur[i >> 3]));
       }
     };
+    if constexpr (!(CAP && BIAS)) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) x[e] = exponent(e);
+      for (int e = 0; e < PER; ++e) {
+        if constexpr (CAP) part[e] = cap_part(s_cur[e]);
+        x[e] = exponent(e, e);
+        if constexpr (CAP) part[e] = cap_part(s_cur[e + PER]);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       s_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[j % RK], qr[j], j == 0 ? z : s_next, 0, 0, 0);
       if (j + RK < NP) kf[j % RK] = k_operand(u, j + RK);
       else if (ahead) kf[j % RK] = k_operand(1, j + RK - NP);
+      if constexpr (BIAS) {
+        if (j == NP / 4) keys = keys_of(CAP ? position : next_position);
+        if (j == NP - 1 && !CAP) add_bias(keys, s_next);
+      }
       weights(2 * j);
       __builtin_amdgcn_sched_barrier(0);
       rs.acc[j % C::MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j % RV], p_prev[j / C::MT], rs.acc[j % C::MT], 0, 0, 0);
@@ -462,7 +536,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       weights(2 * j + 1);
       __builtin_amdgcn_sched_barrier(0);
     }
-    change(u, s_next);
+    if constexpr (CAP && BIAS) position = next_position;
     return sum[0] + sum[1] + w_last;
   };
   // The same for pairs that need a mask or are not seen at all, one part after the other.
@@ -480,6 +554,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       }
     }
     if (see) {
+      if constexpr (CAP) finish(s_cur);
       if (see & 2) {
         // No short-circuits: they become branches on the execution mask, one behind the other for sixteen keys, which took
         // more than the rest of a masked pair (1 000 to 1 600 cycles of it by the clock in the kernel).  Four layers,
@@ -511,7 +586,10 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
         if (j + RK < NP) kf[j % RK] = k_operand(u, j + RK);
         __builtin_amdgcn_sched_barrier(0);
       }
-      change(u, s_next);
+      if constexpr (BIAS) {
+        if (CAP) position = position_of_key(u);
+        else add_bias(keys_of(position_of_key(u)), s_next);
+      }
     }
     see_prev = see;
     see = see_next;
@@ -562,6 +640,34 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int t = 0; t < C::KSTEPS; ++t) asm volatile("" : "+v"(qr[t]));
+  if constexpr (BIAS) {
+    // Scores rise towards the row's own key, and the references after them, at every pair where a head's slope is steep: so a
+    // row starts with the score of its own key, which no other reference has to be below by more than what its weights'
+    // sum may reach, and beside which weights that vanish are nothing.  (A part of the item that does not hold that key has it
+    // all the same.)  Own keys of a wave lie in 32 slots one behind the other: one more tile of scores, and its diagonal.
+    const int first = of_lane(slot, 0), at = min(first + c, slot_hi);
+    const int own_pos = pos_row[slot];
+    const int block = min(max(bt[at / ASPD_BLOCK], 0), a.kv.num_blocks - 1);
+    const u32x4* ksrc = (const u32x4*)((const char*)a.kv.k + ((long)block * a.kv.num_kv_heads + it.h) * C::PAGE_B) +
+                        (at % ASPD_BLOCK) * C::CH + h;
+    bf16x8 own_k[C::KSTEPS];
+#pragma unroll
+    for (int t = 0; t < C::KSTEPS; ++t) own_k[t] = __builtin_bit_cast(bf16x8, ksrc[2 * t]);
+    f32x16 own = z;
+#pragma unroll
+    for (int t = 0; t < C::KSTEPS; ++t) own = __builtin_amdgcn_mfma_f32_32x32x16_bf16(own_k[t], qr[t], own, 0, 0, 0);
+    float r = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r = 8 * (i >> 2) + (i & 3) + 4 * h == slot - first ? own[i] : r;
+    r = over_halves(r, [](float x, float y) { return fmaxf(x, y); });
+    if constexpr (CAP) r = capped(cap_part(r), a.cap_log2);
+    r = fmaf(slope, (float)(own_pos - q_pos), r) * scale;
+    if (fabsf(r) < 0x1p126f) {  // (else as without a bias)
+      rs.m_run = r;
+      rs.neg_ref = -r;
+      rs.limit = ROWS_SUM_MAX;
+    }
+  }
   general_groups(-1, 0);  // (the scores of pair 0)
   int i = 0;
   if (i_open > 0) {
@@ -569,10 +675,16 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       arrive(i, false);
       fetch_first(0);
       float sum = step_full(0, true, s0, s1, p1, p0);
-      if (__any(sum > rs.limit)) sum = rows_raise<D>(s0, rs, p0, scale);
+      if (__any(sum > rs.limit)) {
+        if constexpr (CAP && !BIAS) finish(s0);
+        sum = rows_raise<D>(s0, rs, p0, scale);
+      }
       rs.l_run += sum;
       sum = step_full(1, false, s1, s0, p0, p1);
-      if (__any(sum > rs.limit)) sum = rows_raise<D>(s1, rs, p1, scale);
+      if (__any(sum > rs.limit)) {
+        if constexpr (CAP && !BIAS) finish(s1);
+        sum = rows_raise<D>(s1, rs, p1, scale);
+      }
       rs.l_run += sum;
       next_group(i);
     }

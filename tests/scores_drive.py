@@ -14,8 +14,11 @@ U = 2.0 ** -24
 
 
 def score_error(D, cap):
-    def of(s_abs, s, bias):
-        return U * (D * s_abs + 2 * cap + 8 * (np.abs(s) + np.abs(bias)) + 8)
+    """`spread`: |slope| times how far the positions of a sequence's rows of the step lie apart.  Where many rows are taken
+    together the bias is a sum of two, slope (p_j - p) and slope (p - p_r), p the position of one of the rows: each no larger
+    than |bias| + spread and rounded like it."""
+    def of(s_abs, s, bias, spread):
+        return U * (D * s_abs + 2 * cap + 8 * (np.abs(s) + np.abs(bias) + 2 * spread) + 8)
     return of
 
 
