@@ -265,6 +265,23 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   };
   const int first_branch = !SEQ && a.cu_branches ? load_word_uniform(a.cu_branches + it.s) : 0;
   send(-1);
+  // With a bias: the keys of the wave's own slots, which lie in 32 slots one behind the other, three pages at most, and their
+  // positions (see below).  Between the groups, and their block ids through the scalar path, so that nothing waits for them
+  // but group 0 behind.
+  bf16x8 own_k[BIAS ? C::KSTEPS : 1];
+  int own_pos = 0, own_first = 0;
+  if constexpr (BIAS) {
+    own_first = __builtin_amdgcn_readlane(slot, 0);
+    const int own_last = __builtin_amdgcn_readlane(slot, 31), page = own_first / ASPD_BLOCK, last_page = own_last / ASPD_BLOCK;
+    const int at = min(own_first + c, own_last), in = at / ASPD_BLOCK - page;
+    const int b0 = bt[page], b1 = bt[min(page + 1, last_page)], b2 = bt[min(page + 2, last_page)];
+    const int block = min(max(in == 0 ? b0 : (in == 1 ? b1 : b2), 0), a.kv.num_blocks - 1);
+    const u32x4* src = (const u32x4*)((const char*)a.kv.k + ((long)block * a.kv.num_kv_heads + it.h) * C::PAGE_B) +
+                       (at % ASPD_BLOCK) * C::CH + h;
+    own_pos = pos_row[slot];
+#pragma unroll
+    for (int t = 0; t < C::KSTEPS; ++t) own_k[t] = __builtin_bit_cast(bf16x8, src[2 * t]);
+  }
   if (!l_is_k && l_pair == 0) {  // V of pair -1, which the first full step multiplies with weights zero
 #pragma unroll
     for (int k = 0; k < LPT; ++k) clear_v(0, k);
@@ -437,10 +454,10 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   };
   auto add_bias = [&](bf16x8 keys, f32x16& s) { s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(keys, slopes, s, 0, 0, 0); };
   int position = 0;  // of key lane % 32 of the pair whose weights are next (cap and bias)
-  auto finish = [&](f32x16& s) {  // scores with a cap as they will be, in the log2 domain
+  auto finish = [&](f32x16& s, bf16x8 keys) {  // scores with a cap as they will be, in the log2 domain
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = capped(cap_part(s[i]), a.cap_log2);
-    if constexpr (BIAS) add_bias(keys_of(position), s);
+    if constexpr (BIAS) add_bias(keys, s);
   };
   // Step p (slot u of its group): scores of pair p + 1 (into `s_next`), value products of pair p - 1 (weights `p_prev`),
   // softmax of pair p.  In a full step all three take part.  Its order is written out, one slot per matrix
@@ -543,6 +560,12 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   auto step = [&](int p, int u, const u32x4 (&tn)[2], f32x16& s_cur, f32x16& s_next, const bf16x8 (&p_prev)[2],
                   bf16x8 (&p_cur)[2]) {
     const int see_next = look(p + 1, tn);
+    int next_position = 0;
+    bf16x8 keys;
+    if constexpr (BIAS) {
+      next_position = position_of_key(u);
+      keys = keys_of(CAP ? position : next_position);
+    }
     if (see_prev) {
 #pragma unroll
       for (int t = 0; t < RV; ++t) vf[t] = v_operand(u, t);
@@ -554,7 +577,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       }
     }
     if (see) {
-      if constexpr (CAP) finish(s_cur);
+      if constexpr (CAP) finish(s_cur, keys);
       if (see & 2) {
         // No short-circuits: they become branches on the execution mask, one behind the other for sixteen keys, which took
         // more than the rest of a masked pair (1 000 to 1 600 cycles of it by the clock in the kernel).  Four layers,
@@ -586,11 +609,9 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
         if (j + RK < NP) kf[j % RK] = k_operand(u, j + RK);
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (BIAS) {
-        if (CAP) position = position_of_key(u);
-        else add_bias(keys_of(position_of_key(u)), s_next);
-      }
+      if constexpr (BIAS && !CAP) add_bias(keys, s_next);
     }
+    if constexpr (CAP && BIAS) position = next_position;
     see_prev = see;
     see = see_next;
     tc[0] = tn[0];
@@ -644,21 +665,13 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
     // Scores rise towards the row's own key, and the references after them, at every pair where a head's slope is steep: so a
     // row starts with the score of its own key, which no other reference has to be below by more than what its weights'
     // sum may reach, and beside which weights that vanish are nothing.  (A part of the item that does not hold that key has it
-    // all the same.)  Own keys of a wave lie in 32 slots one behind the other: one more tile of scores, and its diagonal.
-    const int first = of_lane(slot, 0), at = min(first + c, slot_hi);
-    const int own_pos = pos_row[slot];
-    const int block = min(max(bt[at / ASPD_BLOCK], 0), a.kv.num_blocks - 1);
-    const u32x4* ksrc = (const u32x4*)((const char*)a.kv.k + ((long)block * a.kv.num_kv_heads + it.h) * C::PAGE_B) +
-                        (at % ASPD_BLOCK) * C::CH + h;
-    bf16x8 own_k[C::KSTEPS];
-#pragma unroll
-    for (int t = 0; t < C::KSTEPS; ++t) own_k[t] = __builtin_bit_cast(bf16x8, ksrc[2 * t]);
+    // all the same.)  One more tile of scores, and its diagonal.
     f32x16 own = z;
 #pragma unroll
     for (int t = 0; t < C::KSTEPS; ++t) own = __builtin_amdgcn_mfma_f32_32x32x16_bf16(own_k[t], qr[t], own, 0, 0, 0);
     float r = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r = 8 * (i >> 2) + (i & 3) + 4 * h == slot - first ? own[i] : r;
+    for (int i = 0; i < 16; ++i) r = 8 * (i >> 2) + (i & 3) + 4 * h == slot - own_first ? own[i] : r;
     r = over_halves(r, [](float x, float y) { return fmaxf(x, y); });
     if constexpr (CAP) r = capped(cap_part(r), a.cap_log2);
     r = fmaf(slope, (float)(own_pos - q_pos), r) * scale;
@@ -676,13 +689,13 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
       fetch_first(0);
       float sum = step_full(0, true, s0, s1, p1, p0);
       if (__any(sum > rs.limit)) {
-        if constexpr (CAP && !BIAS) finish(s0);
+        if constexpr (CAP && !BIAS) finish(s0, bf16x8{});
         sum = rows_raise<D>(s0, rs, p0, scale);
       }
       rs.l_run += sum;
       sum = step_full(1, false, s1, s0, p0, p1);
       if (__any(sum > rs.limit)) {
-        if constexpr (CAP && !BIAS) finish(s1);
+        if constexpr (CAP && !BIAS) finish(s1, bf16x8{});
         sum = rows_raise<D>(s1, rs, p1, scale);
       }
       rs.l_run += sum;
