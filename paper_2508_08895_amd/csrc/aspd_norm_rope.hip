@@ -2,13 +2,23 @@
 // heads, turn them by positions on several axes, or bias their scores by distance.  Per new token: every query and key head
 // x <- x / sqrt(mean(x^2) + eps) * (offset + w), pair (i, i + D/2) turned by p(axis(i)) * theta^(-2i/D); the query to its
 // row of q_out, the key and the value to the paged cache, the token's position to its slot's entry of slot_pos.
+//
+// Many rows: bound by the bytes, every element read and written once.  Few rows: by the way from the launch over the
+// position and its angles to the stores.  One workgroup per row, as in aspd_rope_append, a lane with the same 16-byte chunks
+// of either half in every head it takes: its cosines, sines and weights are its own in all of them, and the sum of a head's
+// squares goes over as many neighbouring lanes as hold the head.  Units, weights and the slot's entry are on their way before
+// the angles are worked out.  32/8 heads of 128 in bf16 out of one projection, norms of both, in graph replay: 98 997 rows
+// 412 us, 5.9 TB/s (a copy of 2 GiB: 5.0); 7 994 rows on three axes 40 us; 391 rows 4.7 us; three rows of fp32 2.5 us
+// (aspd_rope_append 2.1).  With weights loaded as they are needed, sums by shuffles and the angle's sine in fp64: 445, 41, 4.6 and
+// 2.7.  With half the threads, two units each: 427, 40, 4.6, 3.0; the slot's entry written last: 416, 41, 5.0, 2.9.
+#include <algorithm>
 #include <cmath>
 
 #include "aspd_common.h"
 
 namespace {
 
-constexpr int NR_THREADS = 256;
+constexpr int NR_THREADS = 256;  // at most
 
 template <typename T>
 struct NormRopeArgs {
@@ -34,12 +44,34 @@ struct NormRopeArgs {
   uint32_t       axes[4];       // axis of pair i in bits 2 (i % 16) .. of word i / 16
 };
 
-// Sum over N consecutive lanes (N a power of two); all of them get it.
+// Sum over N consecutive lanes (N a power of two); all of them get it.  Within a row of 16 lanes by data-parallel moves, a
+// shuffle through LDS takes a hundred cycles each.
+template <int CTRL>
+__device__ __forceinline__ float plus_moved(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
 template <int N>
 __device__ __forceinline__ float sum_lanes(float v) {
+  if (N > 1) v = plus_moved<0xb1>(v);    // one further
+  if (N > 2) v = plus_moved<0x4e>(v);    // two further
+  if (N > 4) v = plus_moved<0x141>(v);   // mirrored in the half row
+  if (N > 8) v = plus_moved<0x140>(v);   // mirrored in the row
 #pragma unroll
-  for (int off = N / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  for (int off = 16; off < N; off *= 2) v += __shfl_xor(v, off);
   return v;
+}
+
+// Cosine and sine of p * freq turns.  The product and the distance to the next quarter turn in fp64 (a float product would be
+// 1e-3 rad off at positions of a few ten thousand), the rest, an eighth of a turn at most either way, in fp32: off by 2^-23.
+__device__ __forceinline__ void turn(double p, double freq, float* c, float* s) {
+  const double t = 4.0 * (p * freq - rint(p * freq));
+  const double q = rint(t);
+  float sine, cosine;
+  sincospif(0.5f * (float)(t - q), &sine, &cosine);
+  const int quarter = (int)q & 3;
+  const float a = quarter & 1 ? sine : cosine, b = quarter & 1 ? cosine : sine;
+  *c = quarter == 1 || quarter == 2 ? -a : a;
+  *s = quarter >= 2 ? -b : b;
 }
 
 // VEC pairs per unit: 16 bytes of T from either half of a head, or 1 where a pointer or stride is not a multiple of 16 bytes.
@@ -48,10 +80,10 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
   constexpr int HALF = D / 2;
   constexpr int UPH = HALF / VEC;  // units per head: as many lanes side by side hold a head
   constexpr int U = 2;             // units a thread keeps in flight
-  static_assert(NR_THREADS % UPH == 0 && UPH <= 64, "a thread has the same pairs in every head");
+  static_assert(64 % UPH == 0, "a thread has the same pairs in every head");
   typedef T vec __attribute__((ext_vector_type(VEC)));
   __shared__ __attribute__((aligned(16))) float cs[HALF], sn[HALF];
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, threads = blockDim.x;
   const long row = blockIdx.x;
   const int uq = a.kv.num_q_heads * UPH, uk = a.kv.num_kv_heads * UPH, units = uq + 2 * uk;
   const T* qrow = a.q + row * a.q_stride;
@@ -66,7 +98,7 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
   auto issue = [&](int u0) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = u0 + i * NR_THREADS;
+      const int u = u0 + i * threads;
       if (u >= units) continue;
       const T* src = u < uq ? qrow + u / UPH * D : (u < uq + uk ? krow + (u - uq) / UPH * D : vrow + (u - uq - uk) / UPH * D);
       x[i] = *(const vec*)(src + ch);
@@ -74,18 +106,28 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
     }
   };
   issue(tid);
+  vec wq[2] = {}, wk[2] = {};  // the thread's weights
+  if (a.q_weight) {
+    wq[0] = *(const vec*)(a.q_weight + ch);
+    wq[1] = *(const vec*)(a.q_weight + ch + HALF);
+  }
+  if (a.k_weight) {
+    wk[0] = *(const vec*)(a.k_weight + ch);
+    wk[1] = *(const vec*)(a.k_weight + ch + HALF);
+  }
+  asm volatile("" ::: "memory");  // these loads leave before the angles are worked out
   if (tid < HALF) {
-    double s = 0.0, c = 1.0;
+    float s = 0.f, c = 1.f;
     if (a.log2_theta != 0.0) {
       int p = pos;
       if (a.axis_pos) p = a.axis_pos[(long)((a.axes[tid >> 4] >> (2 * (tid & 15))) & 3) * a.axis_stride + row];
       else if (a.pos_offset) p += a.pos_offset[min(max(a.q_seq[row], 0), a.B - 1)];
-      sincos((double)p * exp2(-(2.0 * tid / D) * a.log2_theta), &s, &c);
+      turn((double)p, exp2(-(2.0 * tid / D) * a.log2_theta) * 0.15915494309189535 /* 1 / 2 pi */, &c, &s);
     }
-    cs[tid] = (float)c;
-    sn[tid] = (float)s;
+    cs[tid] = c;
+    sn[tid] = s;
   }
-  if (a.slot_pos && tid == NR_THREADS - 1) {
+  if (a.slot_pos && tid == threads - 1) {
     const int s = a.q_seq[row], j = a.logical_slot[row];
     if (s >= 0 && s < a.B && j >= 0 && j < a.owner_stride) a.slot_pos[(long)s * a.owner_stride + j] = pos;
   }
@@ -95,7 +137,7 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
   for (int u0 = tid;;) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int u = u0 + i * NR_THREADS;
+      const int u = u0 + i * threads;
       if (u >= units || (u >= uq && !placed)) continue;  // (the lanes of a head go the same way)
       const bool is_q = u < uq, is_v = u >= uq + uk;
       T* dst = is_q ? orow + u / UPH * D
@@ -108,16 +150,15 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
           fa[e] = (float)x[i][e];
           fb[e] = (float)y[i][e];
         }
-        const T* weight = is_q ? a.q_weight : a.k_weight;
-        if (weight) {
+        if (is_q ? a.q_weight : a.k_weight) {
           float sum = 0.f;
 #pragma unroll
           for (int e = 0; e < VEC; ++e) sum += fa[e] * fa[e] + fb[e] * fb[e];
           const float r = rsqrtf(sum_lanes<UPH>(sum) * (1.f / D) + a.eps);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
-            fa[e] *= r * (a.offset + (float)weight[ch + e]);
-            fb[e] *= r * (a.offset + (float)weight[ch + HALF + e]);
+            fa[e] *= r * (a.offset + (float)(is_q ? wq[0][e] : wk[0][e]));
+            fb[e] *= r * (a.offset + (float)(is_q ? wq[1][e] : wk[1][e]));
           }
         }
 #pragma unroll
@@ -130,7 +171,7 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
       *(vec*)(dst + ch) = oa;
       *(vec*)(dst + ch + HALF) = ob;
     }
-    u0 += U * NR_THREADS;
+    u0 += U * threads;
     if (u0 >= units) break;
     issue(u0);
   }
@@ -138,8 +179,11 @@ __global__ __launch_bounds__(NR_THREADS) void norm_rope_append_kernel(NormRopeAr
 
 template <typename T, int D>
 void norm_rope_launch(const NormRopeArgs<T>& a, int rows, bool wide, hipStream_t hs) {
-  if (wide) hipLaunchKernelGGL((norm_rope_append_kernel<T, D, 16 / sizeof(T)>), dim3(rows), dim3(NR_THREADS), 0, hs, a);
-  else hipLaunchKernelGGL((norm_rope_append_kernel<T, D, 1>), dim3(rows), dim3(NR_THREADS), 0, hs, a);
+  // a thread per unit of a row, up to four waves
+  const int vec = wide ? 16 / (int)sizeof(T) : 1, units = (a.kv.num_q_heads + 2 * a.kv.num_kv_heads) * (D / 2 / vec);
+  const int threads = std::min(NR_THREADS, (units + 63) / 64 * 64);
+  if (wide) hipLaunchKernelGGL((norm_rope_append_kernel<T, D, 16 / sizeof(T)>), dim3(rows), dim3(threads), 0, hs, a);
+  else hipLaunchKernelGGL((norm_rope_append_kernel<T, D, 1>), dim3(rows), dim3(threads), 0, hs, a);
 }
 
 template <typename T>
@@ -178,7 +222,7 @@ int norm_rope_append(const aspd_kv* kv, const aspd_state* state, const aspd_step
     for (int i = 0; i < D / 2; ++i) a.axes[i >> 4] |= (uint32_t)how->axis_of_pair[i] << (2 * (i & 15));
   // units of 16 bytes where everything they are read from and written to lies on 16 bytes
   const uintptr_t at = (uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)a.q_out | (uintptr_t)a.kv.k | (uintptr_t)a.kv.v |
-                       (uintptr_t)((a.q_stride | a.k_stride | a.v_stride) * (long)sizeof(T));
+                       (uintptr_t)how->q_weight_d | (uintptr_t)how->k_weight_d | (uintptr_t)((a.q_stride | a.k_stride | a.v_stride) * (long)sizeof(T));
   const bool wide = (at & 15) == 0;
   if (D == 128) norm_rope_launch<T, 128>(a, step->NQ, wide, hs);
   else norm_rope_launch<T, 64>(a, step->NQ, wide, hs);
