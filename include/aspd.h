@@ -358,11 +358,12 @@ ASPD_API int aspd_attn_full_sequence(const aspd_kv* kv, const aspd_state* state,
  * all other arguments, the step's plan and the workspace.  Distances are those of Eq. 4's position ids, so that a branch is
  * biased as if it were alone behind the prefix: slot_pos_d[sequence][slot] holds the position id of the token in each slot
  * that is in use (aspd_norm_rope_append writes it; of slots not in use nothing is used).  Positions and their differences
- * lie within +- 2^24.  Scores are formed in fp32. */
+ * lie within +- 2^24.  Scores are formed in fp32; where many rows are taken together a bias is formed as the sum of two, from
+ * the position of one of the rows, and is off by roundings of slope * (distance of the rows' positions) as well. */
 typedef struct aspd_scores {
   float          softcap;     /* 0: none; otherwise 2^-10 .. 2^10 (ASPD_ERR_UNSUPPORTED outside)                         */
-  const float*   slopes_d;    /* nullable [num_q_heads], finite: usually positive, so that a far key (a negative
-                                 difference) counts less                                                              */
+  const float*   slopes_d;    /* nullable [num_q_heads], usually positive, so that a far key (a negative difference)
+                                 counts less; finite, times any difference and divided by sm_scale too                */
   const int32_t* slot_pos_d;  /* with slopes_d: [B][owner_stride], owner_stride at least max_blocks_per_seq * 16        */
 } aspd_scores;
 ASPD_API int aspd_attn_parallel_decode_scored(const aspd_kv* kv, const aspd_state* state, const aspd_step* step,

@@ -271,14 +271,17 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   bf16x8 own_k[BIAS ? C::KSTEPS : 1];
   int own_pos = 0, own_first = 0;
   if constexpr (BIAS) {
-    own_first = __builtin_amdgcn_readlane(slot, 0);
-    const int own_last = __builtin_amdgcn_readlane(slot, 31), page = own_first / ASPD_BLOCK, last_page = own_last / ASPD_BLOCK;
-    const int at = min(own_first + c, own_last), in = at / ASPD_BLOCK - page;
+    // (slots of rows that the metadata call has refused may hold anything: inside the block table's whatever they say)
+    const int slots_end = a.kv.max_blocks_per_seq * ASPD_BLOCK - 1;
+    own_first = min(max(__builtin_amdgcn_readlane(slot, 0), 0), slots_end);
+    const int own_last = min(max(__builtin_amdgcn_readlane(slot, 31), own_first), slots_end);
+    const int page = own_first / ASPD_BLOCK, last_page = own_last / ASPD_BLOCK;
+    const int at = min(own_first + c, own_last), in = min(at / ASPD_BLOCK - page, 2);
     const int b0 = bt[page], b1 = bt[min(page + 1, last_page)], b2 = bt[min(page + 2, last_page)];
     const int block = min(max(in == 0 ? b0 : (in == 1 ? b1 : b2), 0), a.kv.num_blocks - 1);
     const u32x4* src = (const u32x4*)((const char*)a.kv.k + ((long)block * a.kv.num_kv_heads + it.h) * C::PAGE_B) +
                        (at % ASPD_BLOCK) * C::CH + h;
-    own_pos = pos_row[slot];
+    own_pos = pos_row[min(max(slot, 0), slots_end)];
 #pragma unroll
     for (int t = 0; t < C::KSTEPS; ++t) own_k[t] = __builtin_bit_cast(bf16x8, src[2 * t]);
   }

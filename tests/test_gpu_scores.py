@@ -6,8 +6,9 @@ import torch
 
 import aspd_workloads as W
 from oracle import TokenTable
+from oracle.scores import attend_scored
 from oracle.sequence_layout import replay_layout
-from scores_drive import compare
+from scores_drive import check, compare, score_error, slot_positions
 
 pytestmark = pytest.mark.gpu
 
@@ -126,7 +127,7 @@ def test_whole_sequences(A, hq, hkv, hd, batch, hi, fill, cap, bias):
     wl = W.random_small(31 + hi, num_q_heads=hq, num_kv_heads=hkv, head_dim=hd, batch=batch, prefix_range=(hi // 2, hi))
     layouts = W.random_layouts(wl, seed=hi, fill=fill)
     gb, tt, step, meta = _sequences(A, wl, layouts)
-    rows = None if meta.NQ < 1500 else np.sort(np.random.default_rng(3).choice(meta.NQ, 1500, replace=False))
+    rows = None if meta.NQ < 700 else np.sort(np.random.default_rng(3).choice(meta.NQ, 700, replace=False))
     out, lse, q, scores = compare(A, gb, tt, wl, step, meta, A.aspd_attn_full_sequence, cap, bias, rows=rows, sigma=4.0,
                                   label=f"sequences {hq}/{hkv}x{hd} {hi}")
     again = A.aspd_attn_full_sequence(gb.kv, gb.state, step, q.to(gb.dev), gb.workspace, scores=scores)
@@ -273,3 +274,33 @@ def test_a_grid_of_few_workgroups(A):
     meta = tt.append_parallel(new)
     step = A.aspd_build_branch_meta(gb.kv, gb.state, A.STAGE_PARALLEL, gb._dev_i32(new), NQ=meta.NQ, max_new_per_seq=3, max_workgroups=2)
     compare(A, gb, tt, wl, step, meta, A.aspd_attn_parallel_decode, 10.0, True, sigma=3.0, label="two workgroups")
+
+
+@pytest.mark.parametrize("tokens", [3, 90])     # the streaming, the row-splitting kernel
+def test_rows_of_a_refused_sequence_may_hold_anything(A, tokens):
+    """One sequence of the step outgrows its block table and is refused: its rows of the step keep what was there, and the others
+    are attended as if it were not there."""
+    from gpu_drive import GpuBatch
+    wl = W.random_small(131, num_q_heads=8, num_kv_heads=2, head_dim=128, batch=3, prefix_range=(150, 300))
+    gb = GpuBatch(wl)
+    tt = TokenTable(wl.block_tables, 16)
+    room = [16 * int((row >= 0).sum()) for row in wl.block_tables]
+    have = np.array([room[0] - 100, room[1] - 100, room[2] - 100], dtype=np.int32)
+    tt.append_serial(have)
+    gb.serial(have)
+    new = np.array([tokens, 200, tokens], dtype=np.int32)
+    step = A.Step(int(new.sum()), wl.B, wl.B, gb.dev, max_new_per_seq=200 if tokens > 3 else 6)
+    for t in (step.logical_slot, step.position_ids, step.q_branch, step.kv_len):
+        t.fill_(0x3fffffff)
+    A.aspd_build_branch_meta(gb.kv, gb.state, A.STAGE_SERIAL, gb._dev_i32(new), step=step)
+    assert gb.fault() & A.FAULT_BLOCK_TABLE
+    keep = np.r_[0:tokens, tokens + 200:2 * tokens + 200]
+    meta = tt.append_serial(np.array([tokens, 0, tokens], dtype=np.int32))
+    assert np.array_equal(step.logical_slot.cpu().numpy()[keep], meta.logical_slot)
+    q = wl.draw_q(step.NQ)
+    slopes = np.full(8, 0.05, dtype=np.float32)
+    scores = A.Scores(softcap=10.0, slopes=torch.from_numpy(slopes).to(gb.dev), slot_pos=slot_positions(gb, tt))
+    lse = torch.zeros(step.NQ, 8, device=gb.dev)
+    out = A.aspd_attn_serial_decode(gb.kv, gb.state, step, q.to(gb.dev), gb.workspace, lse=lse, scores=scores)
+    ref = attend_scored(tt, meta, q[keep], wl.k_cache, wl.v_cache, softcap=10.0, slopes=slopes, score_error=score_error(128, 10.0))
+    check(out[keep], lse[keep], ref, "bf16", label=f"beside a refused sequence, {tokens} tokens")
