@@ -19,6 +19,9 @@
 // an unnormalised partial (running max, sum, accumulator); the workgroup that delivers the last partial
 // of an item combines them, in the same launch, or for many rows of few items a launch behind it does (merge_apart).
 //
+// Calls on changed scores (aspd_attn_*_scored: a tanh cap, a bias by the distance of positions) take the same way; a kernel is
+// built once for each of the four combinations.
+//
 // One translation unit: attn_common.h (arguments, plan readers, partial slots), attn_bf16_math.h (what the bf16
 // kernels share: how pages come into LDS and lie there, pieces of the running softmax), attn_bf16_stream.h (the streaming
 // kernel), attn_bf16_rows.h (the row-splitting kernels for chunks and whole sequences), attn_f32.h, attn_merge.h, and the

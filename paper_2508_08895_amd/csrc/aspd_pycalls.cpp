@@ -190,6 +190,27 @@ bool fill(PyObject* obj, aspd_step* out) {
   return f.ok || from_struct(obj, out);
 }
 
+// Of a state its sizes, of a step its rows: all that an append takes of them.
+bool fill_sizes(PyObject* obj, aspd_state* out) {
+  if ((PyObject*)Py_TYPE(obj) != g_state_type) return from_struct(obj, out);
+  memset(out, 0, sizeof(*out));
+  Fields f(obj);
+  f.i32(n_B, &out->B);
+  f.i32(n_owner_stride, &out->owner_stride);
+  return f.ok || from_struct(obj, out);
+}
+bool fill_rows(PyObject* obj, aspd_step* out) {
+  if ((PyObject*)Py_TYPE(obj) != g_step_type) return from_struct(obj, out);
+  memset(out, 0, sizeof(*out));
+  Fields f(obj);
+  f.i32(n_NQ, &out->NQ);
+  f.ptr(n_q_seq, &out->q_seq_d);
+  f.ptr(n_position_ids, &out->position_ids_d);
+  f.ptr(n_logical_slot, &out->logical_slot_d);
+  f.ptr(n_slot_mapping, &out->slot_mapping_d);
+  return f.ok || from_struct(obj, out);
+}
+
 // The address of a tensor (None: null), or of anything else that has data_ptr().
 bool address(PyObject* o, void** out) {
   if (plain_tensor(o)) {
@@ -438,7 +459,7 @@ PyObject* py_norm_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     aspd_rotary how;
     void *q, *k, *v, *q_out = nullptr, *slot_pos, *stream;
     int64_t qs, ks, vs;
-    if (!fill(a[0], &kv) || !fill(a[1], &st) || !fill(a[2], &sp) || !stream_of(a[9], &stream)) return nullptr;
+    if (!fill(a[0], &kv) || !fill_sizes(a[1], &st) || !fill_rows(a[2], &sp) || !stream_of(a[9], &stream)) return nullptr;
     Ref keys_of(PyObject_GetAttr(a[0], n_k));
     const at::Tensor* keys = cache_keys(keys_of);
     if (!keys) return nullptr;

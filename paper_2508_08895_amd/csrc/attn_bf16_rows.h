@@ -136,7 +136,10 @@ struct Result {
   bool complete;
   float* pslot;
 };
-// CAP, BIAS: scores are changed (changed_score) as soon as a pair's are there; `scale` is in them then.
+// CAP, BIAS: changed scores (aspd_scores; see changed_score), in the pair loop's own way.  Plain | cap, bias, both, us: 16-token
+// chunk over 32 sequences of up to 8 192 309 | 373, 322, 396 (720 TFLOP/s of visible keys without, 600 with the cap); 8 whole
+// sequences of 1 100 to 6 000 1 163 | 1 396, 1 169, 1 454; a stage opening over 12 sequences 54 | 62, 61, 69; three whole sequences
+// of up to 1 500 56 | 69, 69, 83.  The cap's instructions bound it: 1.5 times the vector instructions of the plain loop.
 template <int D, int NW, bool SEQ, bool CAP, bool BIAS, typename ResultOf>
 __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const Seg& it, ResultOf result,
                                             int* take_from) {
@@ -413,11 +416,13 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   // ---- changed scores.
   // The cap alone is worked out with the weights: 2 c / (exp(2 s / c) + 1) two slots ahead of them, its constant beside the
   // running reference.
-  // The bias is one more matrix product: of the keys' distances from `base` (the last row's position; 24 bits in three parts
-  // of eight, which bf16 holds exactly) with the slopes (three parts likewise) and of ones with slope * (base - the row's
-  // position), sixteen k-slots in all.  With a cap its result is added to the capped scores, which are written in place;
-  // without one to the products q.k, the slopes divided by sm_scale.  (A subtraction, a conversion and a product-sum for every
-  // score instead: the 64-token chunk 459 us for 312 without a bias, whole sequences 1 561 for 1 193.)
+  // The bias is one more matrix product: of the keys' distances from base_pos, the position of the wave's last row (24 bits in
+  // three parts of eight, which bf16 holds exactly), with the slopes (three parts likewise) and of ones with slope * (base_pos -
+  // the row's position), sixteen k-slots in all.  With a cap its accumulator is the capped scores, written in place; without
+  // one the products q.k, the slopes divided by sm_scale.  (A subtraction, a conversion and a product-sum for every score
+  // instead, and references that go up at every pair: the chunk 459 us for 312 without a bias, whole sequences 1 561 for 1 193.
+  // The operand once per page, by the wave that fetches it, for all: the chunk 346, with a cap 484 for 396, because the loop's
+  // registers are spilled.)
   auto cap_part = [&](float x) -> float { return __builtin_amdgcn_exp2f(x * a.cap_in); };
   auto capped = [&](float part, float constant) -> float {
     return fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(part + 1.f), constant);

@@ -61,8 +61,8 @@ struct AttnArgs {
 
 // A changed score in the log2 domain, sm_scale and log2(e) in it: from the product q.k, the row's slope (times log2(e)) and
 // the key's distance.  c tanh(s / c) = c - 2 c / (exp(2 s / c) + 1): where exp overflows it is c, where it vanishes -c.
-// Fewest instructions (two of them on the slow path of the vector unit); the subtraction leaves an error of 2^-23 c, hence the
-// bound on c: 2^-13 at c = 2^10, a fifth of what the weights' rounding to bf16 is.
+// Five instructions a score, two of them transcendental; the subtraction leaves an error of 2^-23 c, hence the bound on c: 2^-13
+// at c = 2^10, where a weight's rounding to bf16 is 2^-8.
 template <bool CAP, bool BIAS>
 __device__ __forceinline__ float changed_score(const AttnArgs& a, float s, float slope_log2, int distance) {
   float x = CAP ? fmaf(-2.f * a.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * a.cap_in) + 1.f), a.cap_log2)

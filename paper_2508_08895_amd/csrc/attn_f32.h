@@ -34,6 +34,7 @@ __device__ __forceinline__ void halve(float* v, bool upper) {
   }
 }
 
+// CHANGED: changed scores (aspd_scores), cap or bias or both.  A sequence of 91 tokens 8.3 -> 8.6 us.
 template <int D, bool CHANGED>
 __device__ void segment_f32(const AttnArgs& a, char* smem, const Seg& it, bool complete, float* pslot) {
   constexpr int QD = D / 4;        // floats per lane per key
