@@ -281,7 +281,12 @@ def _handles(st):
     st.kv = A.KVCache(st.k_cache, st.v_cache, st.tables, case["hq"])
     st.state = state = A.BatchState(st.B, st.owner.shape[1], dev)
     kind = case["kind"]
-    if kind == "sequences":
+    if kind == "sequences" and case["dtype"] == "f32":
+        # (whole sequences are planned for bf16 attention only: in fp32 a program names the rows of the step itself)
+        st.step = A.Step(st.rows, 0, st.B, dev)
+        for name, rows in (("position_ids", st.pos), ("q_seq", st.q_seq), ("logical_slot", st.slot), ("slot_mapping", st.slot_mapping)):
+            getattr(st.step, name).copy_(rows)
+    elif kind == "sequences":
         runs = [x for r, _ in seqs for x in r]
         st.step = A.aspd_build_sequence_meta(st.kv, state, dev_i32(np.cumsum([0] + [len(r) for r, _ in seqs])),
                                              dev_i32([x[1] for x in runs]), dev_i32([x[3] for x in runs]), st.rows)
