@@ -68,8 +68,8 @@ class _Call:
         self.before = [x.double().cpu().numpy().copy() for x in (self.q, self.k, self.v, *self.pools)]
         self.dtype, self.hd, self.NQ, self.B, self.rng, self.g = dtype, hd, NQ, B, rng, g
 
-    def weight(self):
-        return (1 + 0.3 * torch.randn(self.hd, generator=self.g)).to(_type(self.dtype)).cuda()
+    def weight(self, shift=0):     # `shift` elements off a 16-byte boundary
+        return (1 + 0.3 * torch.randn(self.hd + shift, generator=self.g)).to(_type(self.dtype)).cuda()[shift:]
 
     def check(self, q_got, positions, theta, qw=None, kw=None, offset=0.0, slot_pos=None, eps=EPS):
         q, k, v, kp, vp = self.before
@@ -95,7 +95,7 @@ class _Call:
             assert np.array_equal(slot_pos.cpu().numpy(), table)
 
 
-SHAPES = [("bf16", 32, 8, 128), ("bf16", 6, 6, 64), ("bf16", 7, 1, 128), ("f32", 40, 5, 128), ("f32", 4, 2, 64)]
+SHAPES = [("bf16", 32, 8, 128), ("bf16", 6, 6, 64), ("bf16", 7, 1, 128), ("f32", 40, 5, 128), ("f32", 4, 2, 64), ("bf16", 1, 1, 64)]
 
 
 @pytest.mark.parametrize("dtype,hq,hkv,hd", SHAPES)
@@ -129,7 +129,7 @@ def test_where_the_queries_stand(A, layout):
         c.check(A.aspd_norm_rope_append(c.kv, c.state, c.step, A.Rotary(1e4), c.q, c.k, c.v, q_out=c.q), c.pos, 1e4)
 
 
-@pytest.mark.parametrize("dtype,hq,hkv,hd", SHAPES[:2] + SHAPES[3:])
+@pytest.mark.parametrize("dtype,hq,hkv,hd", SHAPES[:2] + SHAPES[3:5])
 @pytest.mark.parametrize("axes", [1, 2, 3, 4])
 def test_axes(A, dtype, hq, hkv, hd, axes):
     """Sections, turns, and any assignment of pairs to axes; positions of any sign; a wider array than the step's rows."""
@@ -189,6 +189,46 @@ def test_as_aspd_rope_append_without_anything_new(A):
         b.check(b.q, b.pos, 1e6)
         # fp32 arithmetic of the same formula: apart by the roundings of either
         assert (a.q.double() - b.q.double()).abs().max().item() <= (2.0 ** -7 if dtype == "bf16" else 8 * U) * 8
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weights_off_a_boundary(A, dtype):
+    c = _Call(A, dtype, 8, 2, 128, 21, "fused")
+    qw, kw = c.weight(1), c.weight(3)
+    out = torch.empty(21, 8, 128, dtype=_type(dtype), device="cuda")
+    c.check(A.aspd_norm_rope_append(c.kv, c.state, c.step, A.Rotary(1e4, q_weight=qw, k_weight=kw, norm_eps=EPS), c.q, c.k, c.v, q_out=out),
+            c.pos, 1e4, qw, kw)
+
+
+@pytest.mark.parametrize("hq,hkv,hd", [(16, 4, 128), (6, 6, 64)])
+def test_whole_sequences_from_their_tokens(A, hq, hkv, hd):
+    """A re-prefill: metadata of whole sequences, one append, one attention call, on an empty cache."""
+    from gpu_drive import GpuBatch
+    from oracle.sequence_layout import replay_layout
+    from test_gpu_sequence import _build
+    wl = W.random_small(9, num_q_heads=hq, num_kv_heads=hkv, head_dim=hd, batch=3, prefix_range=(60, 300))
+    gb = GpuBatch(wl)
+    gb.kv.k.fill_(float("nan"))
+    gb.kv.v.fill_(float("nan"))
+    layouts = W.random_layouts(wl, seed=4, fill=0.8)
+    tt, meta = replay_layout(wl.block_tables, 16, layouts)
+    step = _build(A, gb, layouts)
+    g = torch.Generator().manual_seed(6)
+    weights, rotary = _chain_rotary(A, wl, g, 1e4)
+    widths = [hq * hd, hkv * hd, hkv * hd]
+    q, k, v = (x.unflatten(1, (-1, hd)) for x in (torch.randn(meta.NQ, sum(widths), generator=g) * 2).bfloat16().cuda().split(widths, 1))
+    slot_pos = A.new_slot_pos(gb.state)
+    q_out = A.aspd_norm_rope_append(gb.kv, gb.state, step, rotary, q, k, v, q_out=torch.empty(meta.NQ, hq, hd, dtype=torch.bfloat16, device="cuda"),
+                                    slot_pos=slot_pos)
+    slopes = (2.0 ** (-8.0 * np.arange(1, hq + 1) / hq)).astype(np.float32)
+    lse = torch.empty(meta.NQ, hq, dtype=torch.float32, device="cuda")
+    out = A.aspd_attn_full_sequence(gb.kv, gb.state, step, q_out, gb.workspace, lse=lse,
+                                    scores=A.Scores(8.0, torch.from_numpy(slopes).cuda(), slot_pos))
+    want = norm_rotate(q.double().cpu().numpy(), meta.position_ids, 1e4, weights[0].double().numpy(), EPS)
+    assert (np.abs(q_out.double().cpu().numpy() - want) <= _bound(want, "bf16")).all()
+    assert np.array_equal(slot_pos.cpu().numpy()[meta.q_seq, meta.logical_slot], meta.position_ids)
+    ref = attend_scored(tt, meta, q_out.cpu(), gb.kv.k.cpu(), gb.kv.v.cpu(), softcap=8.0, slopes=slopes, score_error=score_error(hd, 8.0))
+    check(out, lse, ref, "bf16", label="whole sequences")
 
 
 def test_a_step_without_tokens_and_a_side_stream(A):
