@@ -109,6 +109,7 @@ void set_scores(AttnArgs* a, const aspd_state* state, const aspd_step* step, con
   a->cap_in = cap ? 2.f * a->scale_log2 / scores->softcap : 0.f;
   a->cap_log2 = cap ? scores->softcap * LOG2E : 0.f;
   a->slopes = bias ? scores->slopes_d : nullptr;
+  a->slope_unit = cap ? LOG2E : LOG2E / a->scale_log2;
   a->slot_pos = bias ? scores->slot_pos_d : nullptr;
   a->pos_stride = bias ? state->owner_stride : 0;
   a->position_ids = bias ? step->position_ids_d : nullptr;

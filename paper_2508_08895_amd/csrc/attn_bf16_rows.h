@@ -77,6 +77,12 @@ struct Rows32 {
 // 438 -> 444) and 0.6 % of the 64-sequence ones (chunk 1790 -> 1801 us, whole sequences 23.81 -> 23.94 ms).
 constexpr float ROWS_SUM_MAX = 20.f;
 
+// Pairs of pages from which on a segment with a bias by distance starts from the scores of its rows' own keys (segment_rows): the
+// start is 2 us longer, and no reference goes up afterwards.  Without | with it, us: 300 whole sequences of 40 to 60 tokens (2
+// pairs) 104 | 110, 64 of 200 108 | 110, 40 of 400 (13 at most) 161 | 160, eight prompts of 500 (16) 51 | 54, one of 2 000 (63) 79 | 77,
+// six whole sequences of 4 000 (125) 1 141 | 921.
+constexpr int ROWS_OWN_PAIRS = 24;
+
 // V operand: two transposing reads, eight rows apart.
 template <int D>
 __device__ __forceinline__ bf16x8 rows_v_operand(uint32_t at) {
@@ -240,7 +246,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
     }
     if (BIAS) {
       q_pos = a.position_ids[q];
-      slope = a.slopes[head] * (CAP ? LOG2E : LOG2E / a.scale_log2);  // (added to capped scores, or to products q.k)
+      slope = a.slopes[head] * a.slope_unit;
     }
     const u32x4* qsrc = (const u32x4*)a.q + ((long)q * a.kv.num_q_heads + head) * C::CH + h;
 #pragma unroll
@@ -268,23 +274,20 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   };
   const int first_branch = !SEQ && a.cu_branches ? load_word_uniform(a.cu_branches + it.s) : 0;
   send(-1);
-  // With a bias: the keys of the wave's own slots, which lie in 32 slots one behind the other, three pages at most, and their
-  // positions (see below).  Between the groups, and their block ids through the scalar path, so that nothing waits for them
-  // but group 0 behind.
+  // With a bias: the keys of the wave's own slots, which lie in 32 slots one behind the other, and their positions (see below).
   bf16x8 own_k[BIAS ? C::KSTEPS : 1];
-  int own_pos = 0, own_first = 0;
-  if constexpr (BIAS) {
+  int own_pos = 0, own_index = 0;
+  const bool from_own_key = BIAS && npairs >= ROWS_OWN_PAIRS;
+  if (from_own_key) {
     // (slots of rows that the metadata call has refused may hold anything: inside the block table's whatever they say)
     const int slots_end = a.kv.max_blocks_per_seq * ASPD_BLOCK - 1;
-    own_first = min(max(__builtin_amdgcn_readlane(slot, 0), 0), slots_end);
-    const int own_last = min(max(__builtin_amdgcn_readlane(slot, 31), own_first), slots_end);
-    const int page = own_first / ASPD_BLOCK, last_page = own_last / ASPD_BLOCK;
-    const int at = min(own_first + c, own_last), in = min(at / ASPD_BLOCK - page, 2);
-    const int b0 = bt[page], b1 = bt[min(page + 1, last_page)], b2 = bt[min(page + 2, last_page)];
-    const int block = min(max(in == 0 ? b0 : (in == 1 ? b1 : b2), 0), a.kv.num_blocks - 1);
+    const int first = min(max(__builtin_amdgcn_readlane(slot, 0), 0), slots_end);
+    const int at = min(first + c, min(max(__builtin_amdgcn_readlane(slot, 31), first), slots_end));
+    own_index = slot - first;
+    own_pos = pos_row[min(max(slot, 0), slots_end)];
+    const int block = min(max(a.kv.block_tables[(long)it.s * a.kv.max_blocks_per_seq + at / ASPD_BLOCK], 0), a.kv.num_blocks - 1);
     const u32x4* src = (const u32x4*)((const char*)a.kv.k + ((long)block * a.kv.num_kv_heads + it.h) * C::PAGE_B) +
                        (at % ASPD_BLOCK) * C::CH + h;
-    own_pos = pos_row[min(max(slot, 0), slots_end)];
 #pragma unroll
     for (int t = 0; t < C::KSTEPS; ++t) own_k[t] = __builtin_bit_cast(bf16x8, src[2 * t]);
   }
@@ -669,7 +672,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int t = 0; t < C::KSTEPS; ++t) asm volatile("" : "+v"(qr[t]));
-  if constexpr (BIAS) {
+  if (from_own_key) {
     // Scores rise towards the row's own key, and the references after them, at every pair where a head's slope is steep: so a
     // row starts with the score of its own key, which no other reference has to be below by more than what its weights'
     // sum may reach, and beside which weights that vanish are nothing.  (A part of the item that does not hold that key has it
@@ -679,7 +682,7 @@ __device__ __forceinline__ int segment_rows(const AttnArgs& a, char* smem, const
     for (int t = 0; t < C::KSTEPS; ++t) own = __builtin_amdgcn_mfma_f32_32x32x16_bf16(own_k[t], qr[t], own, 0, 0, 0);
     float r = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) r = 8 * (i >> 2) + (i & 3) + 4 * h == slot - own_first ? own[i] : r;
+    for (int i = 0; i < 16; ++i) r = 8 * (i >> 2) + (i & 3) + 4 * h == own_index ? own[i] : r;
     r = over_halves(r, [](float x, float y) { return fmaxf(x, y); });
     if constexpr (CAP) r = capped(cap_part(r), a.cap_log2);
     r = fmaf(slope, (float)(own_pos - q_pos), r) * scale;

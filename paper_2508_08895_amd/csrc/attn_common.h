@@ -54,6 +54,7 @@ struct AttnArgs {
   // launches on changed scores (aspd_scores), see changed_score
   float          cap_in, cap_log2;       // 2 sm_scale log2(e) / softcap and softcap log2(e); 0: no cap
   const float*   slopes;                 // null: no bias by distance
+  float          slope_unit;             // log2(e) where a bias is added to capped scores, 1 / sm_scale where to products q.k
   const int32_t* slot_pos;
   int            pos_stride;
   const int32_t* position_ids;
