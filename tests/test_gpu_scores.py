@@ -198,6 +198,32 @@ def test_without_a_change_it_is_the_plain_call(A, dtype):
     assert torch.equal(fn(gb.kv, gb.state, step, q, gb.workspace), fn(gb.kv, gb.state, step, q, gb.workspace, scores=A.Scores()))
 
 
+@pytest.mark.parametrize("dtype,new", [("bf16", 1), ("bf16", 17), ("f32", 1)])
+def test_steps_of_serial_and_parallel_sequences(A, dtype, new):
+    """MIXED: branch tokens of two sequences and main-branch tokens of one, a second stage behind a merged one."""
+    from gpu_drive import GpuBatch
+    wl = W.random_small(85, dtype=dtype, num_q_heads=8, num_kv_heads=2, head_dim=128, batch=3, prefix_range=(90, 700), branches_range=(3, 3),
+                        extra_tokens_per_branch=60)
+    gb = GpuBatch(wl)
+    tt = TokenTable(wl.block_tables, 16)
+    tt.append_serial(wl.prefix_len)
+    gb.serial(wl.prefix_len)
+    fn = A.aspd_attn_parallel_decode if new == 1 else A.aspd_attn_branch_chunk
+    for count in ([2, 0, 3], [3, 2, 0]):
+        tt.open_parallel(count)
+        gb.renumber(count)
+        for tokens in (5, new):
+            nb = np.full(sum(count), tokens, dtype=np.int32)
+            nm = np.array([tokens if k == 0 else 0 for k in count], dtype=np.int32)
+            meta = tt.append_mixed(nb, nm)
+            step = gb.mixed(nb, nm)
+            compare(A, gb, tt, wl, step, meta, fn if tokens == new else A.aspd_attn_branch_chunk, 12.0, True, sigma=3.0,
+                    label=f"mixed {dtype} {tokens}")
+        tt.merge()
+        gb.merge()
+    assert gb.fault() == 0
+
+
 def test_a_long_context(A):
     """70 000 tokens: positions and offsets of a long cache, a bias that fades, sampled rows."""
     wl = W.make_workload("long", 91, dtype="bf16", num_q_heads=4, num_kv_heads=1, head_dim=64, sigma=0.5, prefix_range=None,
