@@ -13,6 +13,8 @@ from it.
                   writing that the pins also run against, and the one bench.py times on the host's cores.
   rope.py         rotary encoding of the new tokens by their Eq. 4 position ids and their
                   placement in the cache (the step between the metadata and the attention call).
+  scores.py       attention on capped and distance-biased scores, and the norm and the axes of rotary
+                  positions, with what a bound on their roundings is made of.
 
 Pins (tests/test_oracle_*.py): hand-derived worked example, brute-force visible
 sets, closed-form counts and positions, uniform-weight means, single-key and
